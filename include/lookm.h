@@ -235,6 +235,87 @@ int lookm_decode_step_varlen(const void* q, const void* k_new, const void* v_new
                              const lookm_cache_layout* layout, float* out, void* workspace,
                              size_t workspace_bytes, void* cuda_stream);
 
+/* ---- a paged cache: appending, attention of new tokens, eviction -------------------------------
+ *
+ * What a conversation does over the compressed cache once it goes on: new tokens (a further turn, or
+ * generated ones) join the cache, attend over it, and rows leave it again when it outgrows its budget.
+ * (The paper compresses once, at the prompt; these calls have no counterpart in it beyond Eq. 2-3.)
+ *
+ * K and V live in two pools of pages with the same strides, bf16, head_dim 128.  A page holds page_rows
+ * rows of every KV head (a power of two from 16 to 65536).  Row t of KV head h of request r is at element
+ *     p * page_stride + (t % page_rows) * row_stride + h * head_stride,  p = table[r * table_stride + t / page_rows]
+ * of either pool: [n_pages, n_kv_heads, page_rows, 128] and [n_pages, page_rows, n_kv_heads, 128] pools, or
+ * runs of pages inside a [n_kv_heads, capacity, 128] buffer, into which lookm_compress_layer_opt can write
+ * (lookm_options.out_stride_head).  `mass` is fp32 [n_pages, n_kv_heads, page_rows], contiguous: the attention
+ * weight that every cached row has received.  Strides are multiples of 8 elements, at least 128; pools,
+ * queries and outputs are 16-byte aligned.
+ *
+ * page_table is DEVICE memory, int [n_requests, table_stride]; entries beyond a request's rows are not read.
+ * An entry outside 0 .. n_pages - 1 is never followed: the rows of that page are not written (their keys are read as
+ * zeros), and lookm_device_status() reports LOOKM_ERR_DEVICE_BAD_INDEX.  Requests may share pages that are
+ * only read.
+ *
+ * The status word: these calls raise it and never clear it, so a problem stays reported until
+ * lookm_device_status() has returned it.  Clear a workspace's first 256 bytes once before its first use.
+ *
+ * Query heads share KV heads as in lookm_layout; a group of more than 128 is LOOKM_ERR_UNSUPPORTED. */
+typedef struct {
+    int n_q_heads, n_kv_heads, head_dim;
+    int page_rows, n_pages, table_stride;
+    long long page_stride, row_stride, head_stride;     /* of the K and V pools */
+    long long q_stride_tok, q_stride_head;              /* of the query rows that attend; not used by lookm_evict */
+    float softmax_scale;                                /* 0 selects 1/sqrt(head_dim) */
+} lookm_paged_layout;
+
+/* Bytes of workspace (256-byte aligned) that any of the calls below needs for requests with at most these
+ * numbers of new tokens and cached rows; grows with either, so a workspace for the largest serves all.
+ * new_lens_host may be NULL: one token each.  Returns 0 on invalid arguments. */
+size_t lookm_paged_workspace_size(const lookm_paged_layout* paged, int n_requests, const int* new_lens_host,
+                                  const int* cache_lens_host);
+
+/* What lookm_append_rows does to queries and keys on the way; NULL or an all-zero struct: nothing.
+ *   q_weight, k_weight   device [128] bf16, or NULL: that side is not normed.  y = x / sqrt(mean(x^2) + eps) * weight
+ *                        over the features of a head
+ *   rotary_dim           the first so many features are then turned, in pairs, by position * frequency: 0 (none)
+ *                        or a multiple of 16 up to 128
+ *   interleaved          0: pairs (i, i + rotary_dim / 2); else (2 i, 2 i + 1)
+ *   inv_freq_host        rotary_dim / 2 frequencies in radians per position (host, fp64)
+ * Computed in fp32 with one rounding to bf16 at the end; angles in fp64. */
+typedef struct {
+    const void* q_weight;
+    const void* k_weight;
+    float eps;
+    int rotary_dim, interleaved;
+    const double* inv_freq_host;
+} lookm_append_options;
+
+/* New tokens of a packed ragged batch: request r owns tokens [cu_seqlens_host[r], cu_seqlens_host[r+1])
+ * (zero of them is allowed), which become cache rows cache_lens_host[r], cache_lens_host[r] + 1, ...
+ *   q, k, v     [tokens, heads, 128] bf16 with the strides of `layout`; q and q_out may both be NULL
+ *   positions   device [tokens], may be NULL if rotary_dim is 0
+ *   q_out       the normed and rotated queries, with the q strides of `paged`.  May be q itself if the
+ *               strides are the same; other outputs must not overlap inputs
+ *   mass        set to 0 for the new rows; may be NULL */
+int lookm_append_rows(const void* q, const void* k, const void* v, const int* positions, const int* cu_seqlens_host,
+                      const int* cache_lens_host, int n_requests, const lookm_layout* layout,
+                      const lookm_append_options* options, void* q_out, void* cache_k, void* cache_v, float* mass,
+                      const int* page_table, const lookm_paged_layout* paged, void* workspace, size_t workspace_bytes,
+                      void* cuda_stream);
+
+/* Eviction by accumulated attention weight, per request and KV head: with B = min(budget, len) the last
+ * min(window, B) rows stay and, of the others, the heaviest until there are B (the lower row among equals; NaN counts
+ * as lightest); they become rows 0 .. B - 1 in their order.
+ *   out_k, out_v, out_mass, out_page_table   where the rows go; same layout.  Either the cache itself (in place: the same
+ *               pools, and a table that has the same page at the same place or one that `page_table` does not
+ *               have at all), or pools and pages that overlap none of the input's.  Requests must not share pages that
+ *               are written.  Rows from B on are left as they are.
+ *   kept_idx    receives the row numbers that stayed, in the kept-list layout described at the top (with
+ *               cache_lens_host as lengths).  May be NULL. */
+int lookm_evict(const void* cache_k, const void* cache_v, const float* mass, const int* page_table,
+                const int* cache_lens_host, const int* budgets_host, const int* windows_host, int n_requests,
+                const lookm_paged_layout* paged, void* out_k, void* out_v, float* out_mass, const int* out_page_table,
+                int* kept_idx, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
 /* Byte offsets, inside the workspace, of the intermediate results a whole-path call leaves behind
  * (layouts as described at the top: scores [n_kv_heads, T] fp32, lse [n_q_heads, T] fp32,
  * rank [n_kv_heads, T] i32, kept/evicted/assign lists i32, sim fp32).  They stay valid until

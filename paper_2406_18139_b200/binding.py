@@ -26,6 +26,7 @@ EXPORTS = ["lookm_workspace_size", "lookm_workspace_layout", "lookm_compress_lay
            "lookm_compress_layer_opt", "lookm_compress_varlen_opt", "lookm_score",
            "lookm_select", "lookm_match", "lookm_match_from_sim", "lookm_merge",
            "lookm_decode_workspace_size", "lookm_decode_step", "lookm_decode_step_varlen",
+           "lookm_paged_workspace_size", "lookm_append_rows", "lookm_evict",
            "lookm_set_stage_events", "lookm_selftest_wait_expiry", "lookm_merge_noalloc", "lookm_noalloc_status", "lookm_device_status", "lookm_last_launch_count", "lookm_strerror"]
 N_STAGE_EVENTS = 8
 STAGE_NAMES = ["score_sweep1", "score_sweep2", "select_norms", "gather", "match", "invert", "merge"]
@@ -44,6 +45,18 @@ class CacheLayout(C.Structure):
     _fields_ = [("n_q_heads", C.c_int), ("n_kv_heads", C.c_int), ("head_dim", C.c_int),
                 ("cache_stride_row", C.c_longlong), ("cache_stride_head", C.c_longlong),
                 ("softmax_scale", C.c_float)]
+
+
+class PagedLayout(C.Structure):
+    _fields_ = [("n_q_heads", C.c_int), ("n_kv_heads", C.c_int), ("head_dim", C.c_int),
+                ("page_rows", C.c_int), ("n_pages", C.c_int), ("table_stride", C.c_int),
+                ("page_stride", C.c_longlong), ("row_stride", C.c_longlong), ("head_stride", C.c_longlong),
+                ("q_stride_tok", C.c_longlong), ("q_stride_head", C.c_longlong), ("softmax_scale", C.c_float)]
+
+
+class AppendOptions(C.Structure):
+    _fields_ = [("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("eps", C.c_float), ("rotary_dim", C.c_int),
+                ("interleaved", C.c_int), ("inv_freq_host", C.POINTER(C.c_double))]
 
 
 class Layout(C.Structure):
@@ -84,6 +97,14 @@ def lib():
         L.lookm_decode_step_varlen.argtypes = [vp, vp, vp, vp, vp, C.POINTER(C.c_longlong), ip, C.c_int, cp,
                                                vp, vp, sz, vp]
         L.lookm_decode_step_varlen.restype = C.c_int
+        pp = C.POINTER(PagedLayout)
+        L.lookm_paged_workspace_size.argtypes = [pp, C.c_int, ip, ip]
+        L.lookm_paged_workspace_size.restype = sz
+        L.lookm_append_rows.argtypes = [vp, vp, vp, vp, ip, ip, C.c_int, lp, C.POINTER(AppendOptions), vp, vp, vp, vp, vp, pp,
+                                        vp, sz, vp]
+        L.lookm_append_rows.restype = C.c_int
+        L.lookm_evict.argtypes = [vp, vp, vp, vp, ip, ip, ip, C.c_int, pp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.lookm_evict.restype = C.c_int
         L.lookm_score.argtypes = [vp, vp, ip, C.c_int, lp, vp, vp, C.c_int, vp, sz, vp]
         L.lookm_select.argtypes = [vp, vp, ip, C.c_int, ip, ip, C.c_int, vp, vp, vp, vp, sz, vp]
         L.lookm_match.argtypes = [vp, vp, vp, ip, C.c_int, ip, lp, vp, vp, vp, sz, vp]
@@ -340,6 +361,71 @@ def lookm_decode_step_varlen(q, k_new, v_new, cache_k, cache_v, cache_begin, cac
                                           begins, _ints(cache_lens), len(cache_lens), C.byref(layout),
                                           _ptr(out), _ptr(workspace),
                                           _nbytes(workspace), _stream(stream))
+
+
+def make_paged_layout(q, cache_k, page_table, softmax_scale: float = 0.0, n_q_heads: int = 0) -> PagedLayout:
+    """Layout of a pool seen as [n_pages, n_kv_heads, page_rows, 128] (any strides, last dim contiguous), a table
+    [n_requests, table_stride] and queries [T, Hq, 128].  q may be None (lookm_evict, or a workspace's size) if n_q_heads is given."""
+    assert cache_k.stride(3) == 1 and page_table.stride(1) == 1 and (q is None or q.stride(2) == 1)
+    hq, st, sh = (n_q_heads, 0, 0) if q is None else (q.shape[1], q.stride(0), q.stride(1))
+    # (a dimension of one has any stride: the least that is allowed will do)
+    stride = lambda d: cache_k.stride(d) if cache_k.shape[d] > 1 else max(cache_k.stride(d), 128)
+    table_stride = page_table.stride(0) if page_table.shape[0] > 1 else page_table.shape[1]
+    return PagedLayout(hq, cache_k.shape[1], cache_k.shape[3], cache_k.shape[2], cache_k.shape[0], table_stride, stride(0), stride(2),
+                       stride(1), st, sh, float(softmax_scale))
+
+
+def lookm_paged_workspace_size(paged: PagedLayout, new_lens: Optional[Sequence[int]], cache_lens: Sequence[int]) -> int:
+    return int(lib().lookm_paged_workspace_size(C.byref(paged), len(cache_lens), _ints(new_lens), _ints(cache_lens)))
+
+
+def alloc_paged_workspace(paged: PagedLayout, new_lens, cache_lens, device="cuda"):
+    """A zeroed torch uint8 buffer of lookm_paged_workspace_size bytes."""
+    import torch
+    n = lookm_paged_workspace_size(paged, new_lens, cache_lens)
+    if n == 0:
+        raise ValueError("lookm_paged_workspace_size rejected the layout")
+    return torch.zeros(n, dtype=torch.uint8, device=device)
+
+
+def make_append_options(q_weight=None, k_weight=None, eps: float = 0.0, inv_freq: Optional[Sequence[float]] = None,
+                        interleaved: bool = False) -> AppendOptions:
+    """Options of lookm_append_rows; the first 2 * len(inv_freq) features are rotated.  The weights are bf16 CUDA tensors [128],
+    which the caller keeps alive until the call's work has run."""
+    freq = None if inv_freq is None else (C.c_double * len(inv_freq))(*[float(x) for x in inv_freq])
+    return AppendOptions(_ptr(q_weight), _ptr(k_weight), float(eps), 0 if freq is None else 2 * len(freq), int(bool(interleaved)), freq)
+
+
+def _here(tensors, n: int, page_table, *lists) -> bool:
+    """Whether all tensors are on the current device, where the call would run, and the host lists and the table's rows
+    are as many as the n requests (the library reads them by pointer and can't tell)."""
+    import torch
+    dev = torch._C._cuda_getDevice()
+    return (all(t is None or (t.is_cuda and t.get_device() == dev) for t in tensors) and all(len(x) == n for x in lists)
+            and page_table.dtype == torch.int32 and page_table.shape[0] >= n)
+
+
+def lookm_append_rows(q, k, v, positions, cu_seqlens, cache_lens, layout: Layout, options, q_out, cache_k, cache_v, mass, page_table,
+                      paged: PagedLayout, workspace, stream=None):
+    """options: an AppendOptions (see make_append_options) or None."""
+    n = len(cache_lens)
+    if not _here((q, k, v, positions, q_out, cache_k, cache_v, mass, page_table, workspace), n, page_table, cu_seqlens[1:]):
+        return ERR_INVALID_ARG
+    return lib().lookm_append_rows(_ptr(q), _ptr(k), _ptr(v), _ptr(positions), _ints(cu_seqlens), _ints(cache_lens), n,
+                                   C.byref(layout), None if options is None else C.byref(options), _ptr(q_out), _ptr(cache_k),
+                                   _ptr(cache_v), _ptr(mass), _ptr(page_table), C.byref(paged), _ptr(workspace), _nbytes(workspace),
+                                   _stream(stream))
+
+
+def lookm_evict(cache_k, cache_v, mass, page_table, cache_lens, budgets, windows, paged: PagedLayout, out_k, out_v, out_mass,
+                out_page_table, kept_idx, workspace, stream=None):
+    n = len(cache_lens)
+    if not _here((cache_k, cache_v, mass, page_table, out_k, out_v, out_mass, out_page_table, kept_idx, workspace), n, page_table,
+                 budgets, windows) or out_page_table.dtype != page_table.dtype or out_page_table.shape[0] < n:
+        return ERR_INVALID_ARG
+    return lib().lookm_evict(_ptr(cache_k), _ptr(cache_v), _ptr(mass), _ptr(page_table), _ints(cache_lens), _ints(budgets),
+                             _ints(windows), n, C.byref(paged), _ptr(out_k), _ptr(out_v), _ptr(out_mass),
+                             _ptr(out_page_table), _ptr(kept_idx), _ptr(workspace), _nbytes(workspace), _stream(stream))
 
 
 _stage_event_array = None

@@ -9,14 +9,14 @@
 #include <queue>
 #include <vector>
 
-#include <cudaTypedefs.h>
-
-#include "internal.h"
+#include "host.h"
 
 namespace lookm {
-namespace {
 
 thread_local int g_launches = 0;
+
+namespace {
+
 thread_local void* const* g_stage_events = nullptr;
 
 // Records stage event i of the caller (if per-stage timing is on); errors are ignored on purpose:
@@ -24,8 +24,6 @@ thread_local void* const* g_stage_events = nullptr;
 void mark_stage(int i, cudaStream_t st) {
     if (g_stage_events && g_stage_events[i]) cudaEventRecord(static_cast<cudaEvent_t>(g_stage_events[i]), st);
 }
-
-size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 struct Plan {
     int n_req = 0, n_q_heads = 0, n_kv_heads = 0, group = 1;
@@ -49,9 +47,6 @@ struct Plan {
         o_rnorm_kept, o_assign, o_sim, o_row_begin, o_entries, o_units, o_slot_cnt, o_parts, o_sort_a, o_sort_b,
         total;
 };
-
-struct DeviceInfo { int sms = 0; int cc_major = 0; bool ok = false; };
-int device_info(DeviceInfo& out);
 
 // Blocks per sweep item, from the scores of some 370 problems with one, two and four blocks per item (us).
 // Several blocks pay where there are enough items and the items are full.
@@ -290,6 +285,8 @@ int check_workspace(const Plan& pl, void* ws, size_t bytes) {
     return LOOKM_OK;
 }
 
+}  // namespace
+
 // ---- device facts and the tensor-map encoder ---------------------------------------------------
 int device_info(DeviceInfo& out) {
     static std::mutex mu;
@@ -318,6 +315,8 @@ PFN_cuTensorMapEncodeTiled_v12000 tensor_map_encoder() {
     }();
     return fn;
 }
+
+namespace {
 
 // bf16 tensor [tokens, heads, 128] with element strides; box = 128 tokens x 1 head x 64 features
 // (128 bytes) with the 128-byte swizzle; out-of-range rows read as zero.
@@ -363,24 +362,11 @@ int make_map_2d(CUtensorMap* map, const void* base, long long rows) {
     return r == CUDA_SUCCESS ? LOOKM_OK : LOOKM_ERR_CUDA;
 }
 
-#define LOOKM_CUDA(expr)                                  \
-    do {                                                  \
-        if ((expr) != cudaSuccess) return LOOKM_ERR_CUDA; \
-    } while (0)
-#define LOOKM_TRY(expr)                   \
-    do {                                  \
-        int st_ = (expr);                 \
-        if (st_ != LOOKM_OK) return st_;  \
-    } while (0)
-
 // A whole-path call of one prompt in single blocks needs no table writer: its launches carry the request, and the
 // first of them (sweep 1, or the one that takes its place) clears the words that later ones count in and writes the
 // request to its row, for the launch that reads it there.
 // (Eviction alone, and scores from a given log-sum-exp by themselves, keep it: their callers count five and three launches.)
 bool first_launch_clears(const Plan& pl) { return pl.n_req == 1 && pl.blocks == 1 && pl.splits[0] == 1 && pl.n_none == 0; }
-
-template <class T>
-T* at(void* ws, size_t off) { return reinterpret_cast<T*>(static_cast<char*>(ws) + off); }
 
 // Clears the status word and the arrival counters and writes the request table into the workspace (unless the
 // call's first launch does what is needed of that).

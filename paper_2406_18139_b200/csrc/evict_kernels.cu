@@ -1,0 +1,250 @@
+// Eviction from a paged cache by accumulated attention weight: of the rows 0 .. len - 1 of a (request, KV head) the last
+// `window` stay and the budget - window heaviest of the others, the lower row first among equals; what stays moves to rows
+// 0 .. budget - 1 in its order.
+//
+// evict_select_kernel finds the rows (latency bound: one CTA per (request, KV head), the keys of all candidates in
+// registers), evict_move_kernel moves their keys, values and masses (HBM bound: every kept row read and written once).
+#include <algorithm>
+
+#include "paged.h"
+#include "ptx.cuh"
+
+namespace lookm {
+namespace {
+
+constexpr int kSelThreads = 1024, kSelWarps = kSelThreads / 32;
+
+// Masses in an order that unsigned integers have: -0 as +0, NaN below everything.  Never 0: that is for rows beyond the candidates.
+__device__ __forceinline__ uint32_t key_of(float x) {
+    if (x != x) return 1u;
+    const uint32_t b = __float_as_uint(x + 0.f);
+    return (b & 0x80000000u) ? max(~b, 2u) : b | 0x80000000u;
+}
+
+// Sums of up to three counters over the CTA; two buffers, so that one barrier a call is enough.
+__device__ __forceinline__ void block_sum3(int (&c)[3], int (*buf)[3]) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+    for (int i = 0; i < 3; ++i) c[i] = __reduce_add_sync(0xffffffffu, c[i]);
+    if (lane < 3) buf[warp][lane] = lane == 0 ? c[0] : lane == 1 ? c[1] : c[2];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 3; ++i) c[i] = __reduce_add_sync(0xffffffffu, buf[lane][i]);
+}
+
+// kKeys > 0: so many candidates per thread, whose keys stay in registers; 0: any number, read again in every pass.
+template <int kKeys, int kRequests>
+__global__ void __launch_bounds__(kSelThreads)
+evict_select_kernel(const EvictParams p, const __grid_constant__ Batch<EvictReq, kRequests> batch) {
+    __shared__ int buf[2][kSelWarps][3];
+    __shared__ int2 warp_count[kSelWarps];
+    const EvictReq& rq = batch.r[blockIdx.y];
+    const int h = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int n_cand = rq.len - rq.window, n_top = rq.budget - rq.window;
+    grid_dependency_wait();
+    int* kept = p.kept + rq.kept_off + (long long)h * rq.budget;
+    for (int i = threadIdx.x; i < rq.window; i += kSelThreads) kept[n_top + i] = n_cand + i;
+    if (n_top == n_cand) {                       // nothing leaves
+        for (int i = threadIdx.x; i < n_top; i += kSelThreads) kept[i] = i;
+        return;
+    }
+    if (n_top == 0) return;
+    // every warp has an even share of consecutive rows, one per lane and step
+    const int steps = (n_cand + kSelThreads - 1) / kSelThreads, w0 = warp * steps * 32;
+    const auto read = [&](int s) {
+        const int t = w0 + s * 32 + lane;
+        if (s >= steps || t >= n_cand) return 0u;
+        const int page = p.pages.page_of(rq.index, t, p.status);
+        return page < 0 ? 1u : key_of(__ldg(p.mass + p.pages.mass_at(page, t, h)));
+    };
+    uint32_t key[kKeys > 0 ? kKeys : 1];
+    if constexpr (kKeys > 0) {
+#pragma unroll
+        for (int s = 0; s < kKeys; ++s) key[s] = read(s);
+    }
+    const auto for_each = [&](auto&& f) {
+        if constexpr (kKeys > 0) {
+#pragma unroll
+            for (int s = 0; s < kKeys; ++s) f(s, key[s]);
+        } else {
+            for (int s = 0; s < steps; ++s) f(s, read(s));
+        }
+    };
+    // The n_top-th largest key, two bits a step: the largest x with at least n_top keys >= x.
+    uint32_t x = 0;
+    int turn = 0;
+    for (int bit = 30; bit >= 0; bit -= 2, turn ^= 1) {
+        const uint32_t a = x | (1u << bit), b = x | (2u << bit), c = x | (3u << bit);
+        int n[3] = {0, 0, 0};
+        for_each([&](int, uint32_t k) { n[0] += k >= a; n[1] += k >= b; n[2] += k >= c; });
+        block_sum3(n, buf[turn]);
+        if (n[2] >= n_top) x = c;
+        else if (n[1] >= n_top) x = b;
+        else if (n[0] >= n_top) x = a;
+    }
+    // Rows above it all stay; of those equal to it the lowest that there is room for.
+    int2 mine = {0, 0};                          // above, equal: of the warp
+    for_each([&](int, uint32_t k) {
+        mine.x += __popc(__ballot_sync(0xffffffffu, k > x));
+        mine.y += __popc(__ballot_sync(0xffffffffu, k == x));
+    });
+    if (lane == 0) warp_count[warp] = mine;
+    __syncthreads();
+    int2 c = warp_count[lane];
+    const int above = __reduce_add_sync(0xffffffffu, c.x);
+    if (lane >= warp) c = make_int2(0, 0);
+    const int before_above = __reduce_add_sync(0xffffffffu, c.x);
+    int equal = __reduce_add_sync(0xffffffffu, c.y), at = before_above;
+    const int room = n_top - above;              // for rows equal to x
+    at += min(equal, room);
+    for_each([&](int s, uint32_t k) {
+        const unsigned lower = (1u << lane) - 1u;
+        const unsigned eq = __ballot_sync(0xffffffffu, k == x);
+        const bool stays = k > x || (k == x && equal + __popc(eq & lower) < room);
+        const unsigned all = __ballot_sync(0xffffffffu, stays);
+        if (stays) kept[at + __popc(all & lower)] = w0 + s * 32 + lane;
+        at += __popc(all);
+        equal += __popc(eq);
+    });
+}
+
+constexpr int kMoveThreads = 256;
+constexpr int kMoveRows = 4;                     // of a half-warp at a time
+
+// To pages that share none with the cache's: half a warp per kept row, its key and its value together.
+template <int kRequests>
+__global__ void __launch_bounds__(kMoveThreads)
+evict_copy_kernel(const EvictParams p, const __grid_constant__ Batch<EvictReq, kRequests> batch) {
+    const EvictReq& rq = batch.r[blockIdx.z];
+    const int h = blockIdx.y, l = threadIdx.x & 15;
+    constexpr int kRows = kMoveThreads / 16 * kMoveRows;
+    const int i0 = blockIdx.x * kRows + (threadIdx.x >> 4);
+    if (blockIdx.x * kRows >= rq.budget) return;
+    grid_dependency_wait();
+    const int* kept = p.kept + rq.kept_off + (long long)h * rq.budget;
+    Pages out = p.pages;
+    out.table = p.out_table;
+    uint4 k[kMoveRows], v[kMoveRows];
+    float m[kMoveRows];
+    long long to[kMoveRows], to_mass[kMoveRows];
+    int from[kMoveRows];
+#pragma unroll
+    for (int j = 0; j < kMoveRows; ++j) {
+        const int i = i0 + j * (kMoveThreads / 16);
+        from[j] = i < rq.budget ? kept[i] : -1;
+    }
+#pragma unroll
+    for (int j = 0; j < kMoveRows; ++j) {
+        const int i = i0 + j * (kMoveThreads / 16);
+        to[j] = -1;
+        if (from[j] < 0) continue;
+        const int src = p.pages.page_of(rq.index, from[j], p.status), dst = out.page_of(rq.index, i, p.status);
+        if (src < 0 || dst < 0) continue;
+        const long long at = 2 * p.pages.row_at(src, from[j], h) + l * 16;
+        k[j] = __ldg(reinterpret_cast<const uint4*>(static_cast<const char*>(p.cache_k) + at));
+        v[j] = __ldg(reinterpret_cast<const uint4*>(static_cast<const char*>(p.cache_v) + at));
+        if (l == 0) m[j] = __ldg(p.mass + p.pages.mass_at(src, from[j], h));
+        to[j] = 2 * out.row_at(dst, i, h) + l * 16;
+        to_mass[j] = out.mass_at(dst, i, h);
+    }
+#pragma unroll
+    for (int j = 0; j < kMoveRows; ++j) {
+        if (to[j] < 0) continue;
+        *reinterpret_cast<uint4*>(static_cast<char*>(p.out_k) + to[j]) = k[j];
+        *reinterpret_cast<uint4*>(static_cast<char*>(p.out_v) + to[j]) = v[j];
+        if (l == 0) p.out_mass[to_mass[j]] = m[j];
+    }
+}
+
+// In place.  A CTA takes a slice of 1 / kSlices of the features of all kept rows of one pool's head, in ascending order and a
+// batch at a time: all loads of a batch, a barrier, its stores.  Row i comes from row kept[i] >= i, so a store never
+// hits a row that a later batch still reads, and other CTAs touch other bytes.
+constexpr int kPlaceRows = 8;                    // of a thread at a time
+template <int kSlices, int kRequests>
+__global__ void __launch_bounds__(kMoveThreads)
+evict_in_place_kernel(const EvictParams p, const __grid_constant__ Batch<EvictReq, kRequests> batch) {
+    constexpr int kLanes = 16 / kSlices, kGroups = kMoveThreads / kLanes;        // lanes of a row, rows side by side
+    const EvictReq& rq = batch.r[blockIdx.z];
+    const int h = blockIdx.y, slice = blockIdx.x >> 1;
+    const bool is_v = blockIdx.x & 1, has_mass = blockIdx.x == 0;
+    grid_dependency_wait();
+    const int* kept = p.kept + rq.kept_off + (long long)h * rq.budget;
+    Pages out = p.pages;
+    out.table = p.out_table;
+    const char* in = static_cast<const char*>(is_v ? p.cache_v : p.cache_k);
+    char* to_pool = static_cast<char*>(is_v ? p.out_v : p.out_k);
+    const int l = (slice * kLanes + threadIdx.x % kLanes) * 16;
+    for (int base = 0; base < rq.budget; base += kGroups * kPlaceRows) {
+        uint4 x[kPlaceRows];
+        float m[kPlaceRows];
+        long long to[kPlaceRows], to_mass[kPlaceRows];
+#pragma unroll
+        for (int j = 0; j < kPlaceRows; ++j) {
+            const int i = base + j * kGroups + threadIdx.x / kLanes, from = i < rq.budget ? kept[i] : -1;
+            to[j] = -1;
+            if (from < 0) continue;
+            const int src = p.pages.page_of(rq.index, from, p.status), dst = out.page_of(rq.index, i, p.status);
+            if (src < 0 || dst < 0) continue;
+            x[j] = *reinterpret_cast<const uint4*>(in + 2 * p.pages.row_at(src, from, h) + l);
+            to[j] = 2 * out.row_at(dst, i, h) + l;
+            if (has_mass) {
+                m[j] = p.mass[p.pages.mass_at(src, from, h)];
+                to_mass[j] = out.mass_at(dst, i, h);
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < kPlaceRows; ++j) {
+            if (to[j] < 0) continue;
+            *reinterpret_cast<uint4*>(to_pool + to[j]) = x[j];
+            if (has_mass && threadIdx.x % kLanes == 0) p.out_mass[to_mass[j]] = m[j];
+        }
+    }
+}
+
+template <int kRequests>
+cudaError_t launch(const EvictParams& p, const Batch<EvictReq, kManyRequests>& batch, bool in_place, int num_sms, cudaStream_t stream,
+                   int* launches) {
+    Batch<EvictReq, kRequests> b;
+    b.n = batch.n;
+    b.pad = 0;
+    int candidates = 0, budget = 0;
+    for (int i = 0; i < kRequests; ++i) {
+        b.r[i] = i < batch.n ? batch.r[i] : EvictReq{0, 0, 0, 0, 0};
+        candidates = std::max(candidates, b.r[i].len - b.r[i].window);
+        budget = std::max(budget, b.r[i].budget);
+    }
+    const int heads = p.pages.n_kv_heads;
+    const auto select = candidates <= 2 * kSelThreads    ? evict_select_kernel<2, kRequests>
+                        : candidates <= 8 * kSelThreads  ? evict_select_kernel<8, kRequests>
+                        : candidates <= 32 * kSelThreads ? evict_select_kernel<32, kRequests>
+                                                         : evict_select_kernel<0, kRequests>;
+    cudaError_t err = launch_chained(select, dim3(heads, b.n), dim3(kSelThreads), 0, stream, p, b);
+    if (err != cudaSuccess) return err;
+    ++*launches;
+    if (in_place) {
+        // slices: as many as give every SM a CTA or two
+        const long long units = 2ll * heads * b.n;
+        const int slices = units * 2 >= num_sms * 2 ? 2 : units * 4 >= num_sms * 2 ? 4 : 8;
+        const auto move = slices == 2   ? evict_in_place_kernel<2, kRequests>
+                          : slices == 4 ? evict_in_place_kernel<4, kRequests>
+                                        : evict_in_place_kernel<8, kRequests>;
+        err = launch_chained(move, dim3(2 * slices, heads, b.n), dim3(kMoveThreads), 0, stream, p, b);
+    } else {
+        constexpr int kRows = kMoveThreads / 16 * kMoveRows;
+        err = launch_chained(evict_copy_kernel<kRequests>, dim3((budget + kRows - 1) / kRows, heads, b.n), dim3(kMoveThreads), 0, stream,
+                             p, b);
+    }
+    if (err == cudaSuccess) ++*launches;
+    return err;
+}
+
+}  // namespace
+
+cudaError_t launch_evict(const EvictParams& p, const Batch<EvictReq, kManyRequests>& batch, bool in_place, int num_sms,
+                         cudaStream_t stream, int* launches) {
+    return batch.n <= kFewRequests ? launch<kFewRequests>(p, batch, in_place, num_sms, stream, launches)
+                                   : launch<kManyRequests>(p, batch, in_place, num_sms, stream, launches);
+}
+
+}  // namespace lookm

@@ -1,0 +1,88 @@
+// Internal declarations of the operators over a paged cache: paged_api.cu (host), append_kernel.cu,
+// chunk_kernel.cu, evict_kernels.cu.
+#pragma once
+#include "internal.h"
+
+namespace lookm {
+
+// A paged cache as the kernels see it.  Row t of KV head h of request r is row t % page_rows of page
+// table[r * table_stride + t / page_rows].
+struct Pages {
+    const int* table;
+    int table_stride, n_pages;
+    int page_shift;              // page_rows = 1 << page_shift
+    int n_q_heads, n_kv_heads;
+    long long page_stride, row_stride, head_stride;      // elements of the K and V pools
+#ifdef __CUDACC__
+    // The page of row t of request r; -1 (and *status) if the table names none.
+    __device__ __forceinline__ int page_of(int r, int t, int* status) const {
+        const int p = __ldg(table + (long long)r * table_stride + (t >> page_shift));
+        if (p >= 0 && p < n_pages) return p;
+        atomicMax(status, (int)LOOKM_ERR_DEVICE_BAD_INDEX);
+        return -1;
+    }
+    __device__ __forceinline__ long long row_at(int page, int t, int h) const {
+        return page * page_stride + (t & ((1 << page_shift) - 1)) * row_stride + h * head_stride;
+    }
+    __device__ __forceinline__ long long mass_at(int page, int t, int h) const {
+        return (((long long)page * n_kv_heads + h) << page_shift) + (t & ((1 << page_shift) - 1));
+    }
+#endif
+};
+
+// The requests of a launch, by value (no table in device memory, no copy that would synchronise the host).  A launch takes
+// kFewRequests or kManyRequests of them; longer batches take several launches.
+constexpr int kFewRequests = 16, kManyRequests = 128;
+template <class R, int kRequests>
+struct Batch {
+    int n;
+    int pad;
+    R r[kRequests];
+};
+
+// ---- append_kernel.cu ----------------------------------------------------------------------------
+struct AppendReq {
+    int tok_begin;               // first token on the packed token axis (ascending; the next one's ends it)
+    int row_begin;               // cache row of that token
+    int index;                   // of the request in the page table
+    int pad;
+};
+constexpr int kMaxFreqs = kHeadDim / 2;
+struct AppendParams {
+    Pages pages;
+    const void *q, *k, *v;       // q may be NULL
+    const int* positions;
+    long long q_stride_tok, q_stride_head, kv_stride_tok, kv_stride_head;
+    const void *q_weight, *k_weight;     // [128] bf16 or NULL
+    float eps;
+    int rotary_dim, interleaved;
+    void* q_out;
+    long long qo_stride_tok, qo_stride_head;
+    void *cache_k, *cache_v;
+    float* mass;                 // or NULL
+    int tok_begin, tok_end;      // tokens of this launch
+    int* status;
+    double turns[kMaxFreqs];     // frequencies in turns per position: inv_freq / (2 pi)
+};
+cudaError_t launch_append(const AppendParams& p, const Batch<AppendReq, kManyRequests>& batch, int num_sms, cudaStream_t stream);
+
+// ---- evict_kernels.cu ------------------------------------------------------------------------------
+struct EvictReq {
+    int len, budget, window;     // window <= budget <= len
+    int index;
+    long long kept_off;          // start of its kept lists
+};
+struct EvictParams {
+    Pages pages;
+    const int* out_table;
+    const void *cache_k, *cache_v;
+    const float* mass;
+    void *out_k, *out_v;
+    float* out_mass;
+    int* kept;
+    int* status;
+};
+cudaError_t launch_evict(const EvictParams& p, const Batch<EvictReq, kManyRequests>& batch, bool in_place, int num_sms,
+                         cudaStream_t stream, int* launches);
+
+}  // namespace lookm
