@@ -302,6 +302,27 @@ int lookm_append_rows(const void* q, const void* k, const void* v, const int* po
                       const int* page_table, const lookm_paged_layout* paged, void* workspace, size_t workspace_bytes,
                       void* cuda_stream);
 
+/* Attention of each request's newest tokens over its cache, which holds their own rows already: token i of the
+ * cu_seqlens_host[r+1] - cu_seqlens_host[r] new ones sees rows j <= cache_lens_host[r] - (that many) + i:
+ *     out = softmax(q K^T * scale) V over these rows; what a token does not see has no part in its row
+ * (Eq. 3 for a chunk of tokens.  A whole prompt is a chunk with nothing before it, whose lse lookm_options takes.)
+ *   q     [tokens, n_q_heads, 128] bf16 with the q strides of `paged`; zero tokens of a request are allowed
+ *   out   [tokens, n_q_heads, 128] bf16, contiguous
+ *   lse   [n_q_heads, tokens] fp32, natural-log row log-sum-exp; may be NULL
+ *   cache_lens_host  rows of each cache with the new ones: at least as many as the new tokens
+ * Results do not depend on timing (fixed order of additions). */
+int lookm_chunk_attention(const void* q, const void* cache_k, const void* cache_v, const int* page_table,
+                          const int* cu_seqlens_host, const int* cache_lens_host, int n_requests,
+                          const lookm_paged_layout* paged, void* out, float* lse, void* workspace,
+                          size_t workspace_bytes, void* cuda_stream);
+
+/* The same for one new token per request, which also adds every cached row's softmax weight, summed over the query
+ * heads of its KV head, to the row's mass: what lookm_evict goes by.  q, out [n_requests, n_q_heads, 128],
+ * lse [n_q_heads, n_requests] or NULL; cache_lens_host: at least 1. */
+int lookm_step_attention(const void* q, const void* cache_k, const void* cache_v, float* mass, const int* page_table,
+                         const int* cache_lens_host, int n_requests, const lookm_paged_layout* paged, void* out,
+                         float* lse, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
 /* Eviction by accumulated attention weight, per request and KV head: with B = min(budget, len) the last
  * min(window, B) rows stay and, of the others, the heaviest until there are B (the lower row among equals; NaN counts
  * as lightest); they become rows 0 .. B - 1 in their order.

@@ -26,7 +26,7 @@ EXPORTS = ["lookm_workspace_size", "lookm_workspace_layout", "lookm_compress_lay
            "lookm_compress_layer_opt", "lookm_compress_varlen_opt", "lookm_score",
            "lookm_select", "lookm_match", "lookm_match_from_sim", "lookm_merge",
            "lookm_decode_workspace_size", "lookm_decode_step", "lookm_decode_step_varlen",
-           "lookm_paged_workspace_size", "lookm_append_rows", "lookm_evict",
+           "lookm_paged_workspace_size", "lookm_append_rows", "lookm_chunk_attention", "lookm_step_attention", "lookm_evict",
            "lookm_set_stage_events", "lookm_selftest_wait_expiry", "lookm_merge_noalloc", "lookm_noalloc_status", "lookm_device_status", "lookm_last_launch_count", "lookm_strerror"]
 N_STAGE_EVENTS = 8
 STAGE_NAMES = ["score_sweep1", "score_sweep2", "select_norms", "gather", "match", "invert", "merge"]
@@ -103,6 +103,10 @@ def lib():
         L.lookm_append_rows.argtypes = [vp, vp, vp, vp, ip, ip, C.c_int, lp, C.POINTER(AppendOptions), vp, vp, vp, vp, vp, pp,
                                         vp, sz, vp]
         L.lookm_append_rows.restype = C.c_int
+        L.lookm_chunk_attention.argtypes = [vp, vp, vp, vp, ip, ip, C.c_int, pp, vp, vp, vp, sz, vp]
+        L.lookm_chunk_attention.restype = C.c_int
+        L.lookm_step_attention.argtypes = [vp, vp, vp, vp, vp, ip, C.c_int, pp, vp, vp, vp, sz, vp]
+        L.lookm_step_attention.restype = C.c_int
         L.lookm_evict.argtypes = [vp, vp, vp, vp, ip, ip, ip, C.c_int, pp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.lookm_evict.restype = C.c_int
         L.lookm_score.argtypes = [vp, vp, ip, C.c_int, lp, vp, vp, C.c_int, vp, sz, vp]
@@ -415,6 +419,22 @@ def lookm_append_rows(q, k, v, positions, cu_seqlens, cache_lens, layout: Layout
                                    C.byref(layout), None if options is None else C.byref(options), _ptr(q_out), _ptr(cache_k),
                                    _ptr(cache_v), _ptr(mass), _ptr(page_table), C.byref(paged), _ptr(workspace), _nbytes(workspace),
                                    _stream(stream))
+
+
+def lookm_chunk_attention(q, cache_k, cache_v, page_table, cu_seqlens, cache_lens, paged: PagedLayout, out, lse, workspace, stream=None):
+    n = len(cache_lens)
+    if not _here((q, cache_k, cache_v, page_table, out, lse, workspace), n, page_table, cu_seqlens[1:]):
+        return ERR_INVALID_ARG
+    return lib().lookm_chunk_attention(_ptr(q), _ptr(cache_k), _ptr(cache_v), _ptr(page_table), _ints(cu_seqlens), _ints(cache_lens), n,
+                                       C.byref(paged), _ptr(out), _ptr(lse), _ptr(workspace), _nbytes(workspace), _stream(stream))
+
+
+def lookm_step_attention(q, cache_k, cache_v, mass, page_table, cache_lens, paged: PagedLayout, out, lse, workspace, stream=None):
+    n = len(cache_lens)
+    if not _here((q, cache_k, cache_v, mass, page_table, out, lse, workspace), n, page_table):
+        return ERR_INVALID_ARG
+    return lib().lookm_step_attention(_ptr(q), _ptr(cache_k), _ptr(cache_v), _ptr(mass), _ptr(page_table), _ints(cache_lens), n,
+                                      C.byref(paged), _ptr(out), _ptr(lse), _ptr(workspace), _nbytes(workspace), _stream(stream))
 
 
 def lookm_evict(cache_k, cache_v, mass, page_table, cache_lens, budgets, windows, paged: PagedLayout, out_k, out_v, out_mass,

@@ -1,0 +1,745 @@
+// Attention of each request's newest tokens over its paged cache, causal among themselves:
+//
+//     s_ij = q_i . k_j * scale  for rows j <= len - n_new + i,   out_i = sum_j softmax(s_i)_j v_j
+//
+// chunk_kernel: persistent, one CTA per SM.  Two streams of work run side by side, each with a 128 x 128 fp32 block of logits
+// and one of outputs in tensor memory (all 512 columns) and a warpgroup that turns logits into probabilities; while one
+// warpgroup works, the tensor core multiplies for the other.  An item is one KV head of one request with
+//   two query tiles (128 rows each: tokens x query heads of the group): both streams meet every tile of 128 cached rows, or
+//   one query tile: the streams take the cached rows' tiles alternately and are added up at the end,
+// over all rows that these tokens see or over a range of them (few items: the ranges are added up by chunk_finish_kernel).
+//   warps 0-3, 4-7  softmax of stream 0 and 1: a thread has a row of logits.  Probabilities become bf16 (the type of V, which
+//                   the tensor core wants on both sides: an error of at most 2^-8 each that averages out over the row's sum, no larger than the output's own
+//                   rounding) and lie where the logits lay, as the A operand of P V.  Sums stay fp32.  The reference that is subtracted follows the
+//                   maximum only when that has grown by 2^8, so outputs are seldom rescaled
+//   warp 8          query tiles and cached rows by TMA, page by page, into one ring of tiles for K and V alternately
+//   warp 9          issues the MMAs: S = Q K^T, O += P V.  They run in the order they are issued in, so the next S may
+//                   overwrite the P that the product before it reads
+//   warps 10-11     V rows that not every row of the item sees: what lies behind the cache's end becomes zero, and so do infinities and
+//                   NaN (0 times which would be NaN in rows that don't see them); rows that do see them get them in the epilogue
+#include <algorithm>
+
+#include <cuda_bf16.h>
+#include <math.h>
+
+#include "paged.h"
+#include "ptx.cuh"
+
+namespace lookm {
+namespace {
+
+constexpr int kSoftmaxWarps = 8, kLoadWarp = 8, kMmaWarp = 9, kCleanWarp = 10;
+constexpr int kThreads = 384;
+constexpr int kHalfBytes = kTile * 64 * 2, kTileBytes = 2 * kHalfBytes;
+constexpr int kRing = 5;
+constexpr int kFlags = 4;                        // items between a flag's uses: more than the ring lets the loads run ahead
+constexpr int kSoftmaxRegs = 216, kOtherRegs = 72;
+static_assert(256 * kSoftmaxRegs + 128 * kOtherRegs <= 65536 / kThreads / 8 * 8 * kThreads, "register shares exceed the launch's");
+constexpr float kRescaleAt = 8.f;                // log2 of the growth of a row's maximum at which its reference follows
+
+struct __align__(1024) ChunkShared {
+    uint8_t q[2][kTileBytes];
+    uint8_t ring[kRing][kTileBytes];
+    float merge_m[kTile], merge_l[kTile];        // one query tile: stream 1's reference and sum
+    unsigned long long q_full[2], q_empty[2];
+    unsigned long long full[kRing], empty[kRing];
+    unsigned long long dirty[kRing];             // V tiles that warps 10 and 11 have to look at; they make them full
+    unsigned long long s_full[2], p_full[2], pv_done[2], o_free[2];
+    unsigned long long merge_full, merge_free, mma_done;
+    int odd_values[kFlags];                      // V had infinities or NaN that were taken out
+    uint32_t tmem_base;
+    int abort_flag;
+};
+static_assert(sizeof(ChunkShared) + 1024 <= 232448, "shared memory exceeds 227 KB");
+
+struct Item {
+    int q_begin, n_new, len, index, head, split;
+    int tok0;                                    // of its first query tile
+    bool pair;                                   // two query tiles
+    bool partial;                                // a range of the rows
+    int t0;                                      // first tile of cached rows
+    int nt, nt0, nt1;                            // tiles of cached rows: all (loaded), of stream 0, of stream 1
+    int min_seen;                                // cached rows that its first token sees: every row of the item sees these
+    long long part_begin, logits_begin;
+};
+
+template <int kRequests>
+__device__ __forceinline__ Item decode_item(const ChunkParams& p, const Batch<ChunkReq, kRequests>& batch, int item) {
+    int lo = 0, hi = batch.n - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (batch.r[mid].item_begin <= item) lo = mid; else hi = mid - 1;
+    }
+    const ChunkReq& rq = batch.r[lo];
+    int u = item - rq.item_begin;
+    Item it;
+    it.head = u % p.pages.n_kv_heads;
+    u /= p.pages.n_kv_heads;
+    it.split = u % rq.splits;
+    const int set = rq.n_sets - 1 - u / rq.splits;           // those that see most rows first
+    it.q_begin = rq.q_begin;
+    it.n_new = rq.n_new;
+    it.len = rq.len;
+    it.index = rq.index;
+    it.tok0 = set * 2 * p.tile_tokens;
+    it.pair = it.tok0 + p.tile_tokens < rq.n_new;
+    it.partial = rq.splits > 1;
+    it.part_begin = rq.part_begin;
+    it.logits_begin = rq.logits_begin;
+    const int before = rq.len - rq.n_new;
+    it.min_seen = before + it.tok0 + 1;
+    const int seen0 = before + min(rq.n_new, it.tok0 + p.tile_tokens), seen1 = before + min(rq.n_new, it.tok0 + 2 * p.tile_tokens);
+    const int tiles0 = (seen0 + kTile - 1) / kTile, tiles = it.pair ? (seen1 + kTile - 1) / kTile : tiles0;
+    it.t0 = (int)((long long)tiles * it.split / rq.splits);
+    it.nt = (int)((long long)tiles * (it.split + 1) / rq.splits) - it.t0;
+    if (it.pair) {
+        it.nt1 = it.nt;
+        it.nt0 = min(max(tiles0 - it.t0, 0), it.nt);
+    } else {
+        it.nt0 = (it.nt + 1) >> 1;
+        it.nt1 = it.nt >> 1;
+    }
+    return it;
+}
+// Serpentine deal of the items; -1: a round in which this CTA has none
+__device__ __forceinline__ int item_of_round(int round, int n_items) {
+    const int n = gridDim.x, item = round * n + ((round & 1) ? n - 1 - (int)blockIdx.x : (int)blockIdx.x);
+    return item < n_items ? item : -1;
+}
+// Whether some row of the item does not see all 128 rows of tile t (or the cache ends in it).
+__device__ __forceinline__ bool is_masked(const Item& it, int t) { return (it.t0 + t + 1) * kTile > it.min_seen; }
+
+// The waits of a warp: all lanes wait, and all follow one verdict.
+__device__ __forceinline__ bool warp_wait(unsigned long long* bar, uint32_t parity, volatile int* abort_flag) {
+    return __all_sync(0xffffffffu, ptx::mbar_wait(ptx::smem_u32(bar), parity, abort_flag));
+}
+
+__device__ __forceinline__ bool odd_bf16(uint32_t x) { return (x & 0x7f80u) == 0x7f80u; }     // infinity or NaN
+
+// ---- warp 8 ---------------------------------------------------------------------------------------
+template <int kRequests>
+__device__ __forceinline__ void load_tiles(const CUtensorMap& map_q, const CUtensorMap& map_k, const CUtensorMap& map_v,
+                                           const ChunkParams& p, const Batch<ChunkReq, kRequests>& batch, ChunkShared& sh) {
+    const int lane = threadIdx.x & 31, rounds = (p.n_items + gridDim.x - 1) / gridDim.x;
+    volatile int* abort_flag = &sh.abort_flag;
+    if (lane == 0) {
+        ptx::prefetch_tensormap(&map_q);
+        ptx::prefetch_tensormap(&map_k);
+        ptx::prefetch_tensormap(&map_v);
+    }
+    const int box_rows = min(1 << p.pages.page_shift, kTile), boxes = kTile / box_rows;
+    const int q_bytes = p.tile_tokens * p.group * 256;
+    uint32_t n = 0, nq = 0;                      // tiles and query tiles armed so far
+    uint32_t dirty_phase = 0, last_dirty = 0;    // per stage: parity of its next use as a dirty one, whether its last use was one
+    bool stop = false;
+    for (int round = 0; round < rounds && !stop; ++round) {
+        const int item = item_of_round(round, p.n_items);
+        if (item < 0) continue;
+        const Item it = decode_item(p, batch, item);
+        if (it.nt == 0) continue;                // (a set that sees fewer tiles than there are ranges)
+        for (int g = 0; g < (it.pair ? 2 : 1) && !stop; ++g, ++nq) {
+            const int s = nq & 1;
+            if (!warp_wait(&sh.q_empty[s], ((nq >> 1) & 1) ^ 1, abort_flag)) { stop = true; break; }
+            if (lane == 0) {
+                const uint32_t bar = ptx::smem_u32(&sh.q_full[s]), dst = ptx::smem_u32(&sh.q[s][0]);
+                const int tok = it.q_begin + it.tok0 + g * p.tile_tokens;
+                ptx::mbar_arrive_expect_tx(bar, q_bytes);
+                ptx::tma_load_3d(dst, &map_q, 0, it.head * p.group, tok, bar);
+                ptx::tma_load_3d(dst + kHalfBytes, &map_q, 64, it.head * p.group, tok, bar);
+            }
+        }
+        const auto load = [&](const CUtensorMap& map, int t, bool dirty) {
+            if (stop) return;
+            const int s = n % kRing, row = (it.t0 + t) * kTile + lane * box_rows;
+            int page = p.pages.n_pages;          // beyond the pool: reads as zeros
+            if (lane < boxes && row < it.len) {
+                page = p.pages.page_of(it.index, row, p.status);
+                if (page < 0) page = p.pages.n_pages;
+            }
+            if (!warp_wait(&sh.empty[s], ((n / kRing) & 1) ^ 1, abort_flag)) { stop = true; return; }
+            const uint32_t bar = ptx::smem_u32(dirty ? &sh.dirty[s] : &sh.full[s]);
+            if (lane == 0) {
+                ptx::mbar_arrive_expect_tx(bar, kTileBytes);
+                if (!dirty) ptx::mbar_arrive(bar);           // (the cleaning warps are two)
+            }
+            last_dirty = (last_dirty & ~(1u << s)) | (dirty ? 1u << s : 0u);
+            if (dirty) dirty_phase ^= 1u << s;
+            __syncwarp();
+            if (lane < boxes) {
+                const uint32_t dst = ptx::smem_u32(&sh.ring[s][0]) + lane * box_rows * 128;
+                const int in_page = row & ((1 << p.pages.page_shift) - 1);
+                ptx::tma_load_4d(dst, &map, 0, in_page, it.head, page, bar);
+                ptx::tma_load_4d(dst + kHalfBytes, &map, 64, in_page, it.head, page, bar);
+            }
+            ++n;
+        };
+        if (it.pair) {
+            load(map_k, 0, false);
+            for (int t = 0; t < it.nt && !stop; ++t) {
+                load(map_v, t, is_masked(it, t));
+                if (t + 1 < it.nt) load(map_k, t + 1, false);
+            }
+        } else {
+            load(map_k, 0, false);
+            if (it.nt > 1) load(map_k, 1, false);
+            for (int t = 0; t < it.nt && !stop; ++t) {
+                load(map_v, t, is_masked(it, t));
+                if (t + 2 < it.nt) load(map_k, t + 2, false);
+            }
+        }
+    }
+    // After an abort: no copy may write shared memory once the CTA has left (bounded, the flag is ignored).
+    if (*abort_flag && lane == 0) {
+        int ignore = 0;
+        for (uint32_t i = n > (uint32_t)kRing ? n - kRing : 0; i < n; ++i)
+            if (last_dirty >> (i % kRing) & 1)
+                ptx::mbar_wait(ptx::smem_u32(&sh.dirty[i % kRing]), (dirty_phase >> (i % kRing) & 1) ^ 1, &ignore, 200000000ull);
+            else
+                ptx::mbar_wait(ptx::smem_u32(&sh.full[i % kRing]), (i / kRing) & 1, &ignore, 200000000ull);
+        for (uint32_t i = nq > 2u ? nq - 2 : 0; i < nq; ++i)
+            ptx::mbar_wait(ptx::smem_u32(&sh.q_full[i & 1]), (i >> 1) & 1, &ignore, 200000000ull);
+    }
+    __syncwarp();
+}
+
+// ---- warp 9, one thread ---------------------------------------------------------------------------
+template <int kRequests>
+__device__ __forceinline__ void issue_mmas(const ChunkParams& p, const Batch<ChunkReq, kRequests>& batch, ChunkShared& sh, uint32_t tmem) {
+    const int rounds = (p.n_items + gridDim.x - 1) / gridDim.x;
+    volatile int* abort_flag = &sh.abort_flag;
+    constexpr uint32_t idesc_s = ptx::umma_idesc_bf16(kTile, kTile), idesc_o = ptx::umma_idesc_bf16(kTile, kHeadDim) | ptx::kIdescBMnMajor;
+    uint32_t n = 0, nq = 0;
+    uint32_t np[2] = {0, 0}, no[2] = {0, 0};     // tiles and items of a stream so far
+    bool stop = false;
+    const auto wait = [&](unsigned long long* bar, uint32_t parity) {
+        if (!stop && !ptx::mbar_wait(ptx::smem_u32(bar), parity, abort_flag)) stop = true;
+    };
+    for (int round = 0; round < rounds && !stop; ++round) {
+        const int item = item_of_round(round, p.n_items);
+        if (item < 0) continue;
+        const Item it = decode_item(p, batch, item);
+        if (it.nt == 0) continue;
+        const int tiles = it.pair ? 2 : 1;
+        for (int g = 0; g < tiles; ++g) wait(&sh.q_full[(nq + g) & 1], ((nq + g) >> 1) & 1);
+        const auto qk = [&](int g, uint32_t stage) {             // S of stream g = its query tile x K^T
+            if (stop) return;
+            const uint32_t a = ptx::smem_u32(&sh.q[(nq + (it.pair ? g : 0)) & 1][0]), b = ptx::smem_u32(&sh.ring[stage][0]);
+#pragma unroll
+            for (int kk = 0; kk < 8; ++kk) {
+                const uint32_t off = (kk >> 2) * kHalfBytes + (kk & 3) * 32;
+                ptx::umma_bf16(tmem + g * kTile, ptx::umma_desc_sw128(a + off), ptx::umma_desc_sw128(b + off), idesc_s, kk > 0);
+            }
+            ptx::umma_commit(ptx::smem_u32(&sh.s_full[g]));
+        };
+        bool fresh[2] = {true, true};            // the stream's output block has nothing of this item yet
+        const auto pv = [&](int g, uint32_t stage) {             // O of stream g += P x V
+            wait(&sh.p_full[g], np[g] & 1);
+            if (stop) return;
+            ++np[g];
+            ptx::tc_fence_after_sync();
+            const uint32_t b = ptx::smem_u32(&sh.ring[stage][0]);
+#pragma unroll
+            for (int kk = 0; kk < 8; ++kk)
+                ptx::umma_bf16_ts(tmem + 2 * kTile + g * kHeadDim, tmem + g * kTile + kk * 8,
+                                  ptx::umma_desc_sw128_mn(b + kk * 2048, kHalfBytes), idesc_o, kk > 0 || !fresh[g]);
+            fresh[g] = false;
+            ptx::umma_commit(ptx::smem_u32(&sh.pv_done[g]));
+        };
+        const auto arrived = [&] {               // the next tile of the ring
+            const uint32_t s = n % kRing;
+            wait(&sh.full[s], (n / kRing) & 1);
+            ++n;
+            if (!stop) ptx::tc_fence_after_sync();
+            return s;
+        };
+        const auto release = [&](uint32_t s) { if (!stop) ptx::umma_commit(ptx::smem_u32(&sh.empty[s])); };
+        const auto queries_done = [&] {
+            for (int g = 0; g < tiles && !stop; ++g) ptx::umma_commit(ptx::smem_u32(&sh.q_empty[(nq + g) & 1]));
+        };
+        // the output blocks are free when the epilogue of the item before has read them
+        const auto outputs_free = [&] {
+            if (it.nt0 > 0) wait(&sh.o_free[0], (no[0]++ & 1) ^ 1);
+            if (it.nt1 > 0) wait(&sh.o_free[1], (no[1]++ & 1) ^ 1);
+        };
+        if (it.pair) {
+            uint32_t k = arrived();
+            if (it.nt0 > 0) qk(0, k);
+            qk(1, k);
+            release(k);
+            if (it.nt == 1) queries_done();
+            outputs_free();
+            for (int t = 0; t < it.nt && !stop; ++t) {
+                const uint32_t v = arrived();
+                if (t < it.nt0) pv(0, v);
+                if (t + 1 < it.nt) {
+                    k = arrived();
+                    if (t + 1 < it.nt0) qk(0, k);
+                }
+                pv(1, v);
+                release(v);
+                if (t + 1 < it.nt) {
+                    qk(1, k);
+                    release(k);
+                    if (t + 2 == it.nt) queries_done();
+                }
+            }
+        } else {
+            for (int t = 0; t < min(it.nt, 2); ++t) {
+                const uint32_t k = arrived();
+                qk(t, k);
+                release(k);
+            }
+            if (it.nt <= 2) queries_done();
+            outputs_free();
+            for (int t = 0; t < it.nt && !stop; ++t) {
+                const uint32_t v = arrived();
+                pv(t & 1, v);
+                release(v);
+                if (t + 2 < it.nt) {
+                    const uint32_t k = arrived();
+                    qk(t & 1, k);
+                    release(k);
+                    if (t + 3 == it.nt) queries_done();
+                }
+            }
+        }
+        nq += tiles;
+    }
+    int ignore = 0;                              // no MMA may be running when TMEM is released
+    ptx::umma_commit(ptx::smem_u32(&sh.mma_done));
+    ptx::mbar_wait(ptx::smem_u32(&sh.mma_done), 0, &ignore, 1000000000ull);
+}
+
+// ---- warps 10 and 11 --------------------------------------------------------------------------------
+template <int kRequests>
+__device__ __forceinline__ void clean_values(const ChunkParams& p, const Batch<ChunkReq, kRequests>& batch, ChunkShared& sh) {
+    const int lane = threadIdx.x & 31, half = (threadIdx.x >> 5) - kCleanWarp, rounds = (p.n_items + gridDim.x - 1) / gridDim.x;
+    volatile int* abort_flag = &sh.abort_flag;
+    uint32_t n = 0, n_items = 0, phase = 0;
+    for (int round = 0; round < rounds; ++round) {
+        const int item = item_of_round(round, p.n_items);
+        if (item < 0) continue;
+        const Item it = decode_item(p, batch, item);
+        if (it.nt == 0) continue;
+        for (int t = 0; t < it.nt; ++t) {
+            // the ring position of V tile t: K and V take turns, with one K tile ahead, or two with one query tile
+            const uint32_t at = n + (it.pair ? 2 * t + 1 : t < it.nt - 1 ? 2 * t + 2 : 2 * t + 1);
+            if (!is_masked(it, t)) continue;
+            const uint32_t s = at % kRing;
+            if (!warp_wait(&sh.dirty[s], (phase >> s) & 1, abort_flag)) return;
+            phase ^= 1u << s;
+            const int row0 = (it.t0 + t) * kTile;
+            const int end = min(max(it.len - row0, 0), kTile), all_see = min(max(it.min_seen - row0, 0), kTile);
+            uint4* v = reinterpret_cast<uint4*>(&sh.ring[s][half * kHalfBytes]);      // [128 rows][8]; within a row any order
+            for (int i = end * 8 + lane; i < kTile * 8; i += 32) v[i] = make_uint4(0, 0, 0, 0);
+            bool odd = false;
+            for (int i = all_see * 8 + lane; i < end * 8; i += 32) {
+                uint4 x = v[i];
+                uint32_t* w = reinterpret_cast<uint32_t*>(&x);
+                bool here = false;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (odd_bf16(w[j])) { w[j] &= 0xffff0000u; here = true; }
+                    if (odd_bf16(w[j] >> 16)) { w[j] &= 0xffffu; here = true; }
+                }
+                if (here) { v[i] = x; odd = true; }
+            }
+            if (odd) sh.odd_values[n_items % kFlags] = (int)n_items + 1;
+            ptx::fence_proxy_async_shared();
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&sh.full[s]));
+        }
+        n += 2 * it.nt;
+        ++n_items;
+    }
+}
+
+// ---- warps 0 to 7 ------------------------------------------------------------------------------------
+template <int kRequests, bool kStep>
+__device__ __forceinline__ void softmax_rows(const ChunkParams& p, const Batch<ChunkReq, kRequests>& batch, ChunkShared& sh, uint32_t tmem) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = warp >> 2, row = (warp & 3) * 32 + lane;
+    const int rounds = (p.n_items + gridDim.x - 1) / gridDim.x;
+    volatile int* abort_flag = &sh.abort_flag;
+    const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const uint32_t ts = tmem + g * kTile + lanes, to = tmem + 2 * kTile + g * kHeadDim + lanes;
+    const float c = p.scale_log2;
+    const int tok_in_tile = row / p.group, head_in_group = row - tok_in_tile * p.group;
+    uint32_t n = 0, n_items = 0, n_merges = 0;
+    for (int round = 0; round < rounds; ++round) {
+        const int item = item_of_round(round, p.n_items);
+        if (item < 0) continue;
+        const Item it = decode_item(p, batch, item);
+        const int tok = it.tok0 + (it.pair ? g * p.tile_tokens : 0) + tok_in_tile;
+        const bool live = tok_in_tile < p.tile_tokens && tok < it.n_new;
+        const bool any_live = __any_sync(0xffffffffu, live);
+        const int seen = live ? it.len - it.n_new + tok + 1 : 0x7fffffff;
+        const int nt = g ? it.nt1 : it.nt0;
+        const int q_head = it.head * p.group + head_in_group;
+        const long long part_row = it.part_begin + ((long long)it.split * it.n_new + tok) * p.pages.n_q_heads + q_head;
+        if (it.nt == 0) {                        // a range of nothing: no role does anything for it
+            if (live && (it.pair || g == 0)) p.part_lse[part_row] = -INFINITY;
+            continue;
+        }
+        float m = -INFINITY, l = 0.f;
+        for (int j = 0; j < nt; ++j, ++n) {
+            const int t = it.t0 + (it.pair ? j : 2 * j + g);
+            if (!warp_wait(&sh.s_full[g], n & 1, abort_flag)) return;
+            if (any_live) {
+                ptx::tc_fence_after_sync();
+                uint32_t s[4][32];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) ptx::tmem_ld_32x32(ts + i * 32, s[i]);
+                ptx::tmem_ld_wait();
+                if constexpr (kStep) {
+                    if (live) {
+                        float* to_logits = p.logits + it.logits_begin + (long long)(it.head * p.group + head_in_group) * it.len + t * kTile;
+                        const int cols = min(kTile, it.len - t * kTile);
+#pragma unroll
+                        for (int i = 0; i < kTile; ++i)
+                            if (i < cols) to_logits[i] = __uint_as_float(s[i >> 5][i & 31]);
+                    }
+                }
+                const int cols = seen - t * kTile;
+                if (__any_sync(0xffffffffu, cols < kTile)) {
+#pragma unroll
+                    for (int i = 0; i < kTile; ++i)
+                        if (i >= cols) s[i >> 5][i & 31] = __float_as_uint(-INFINITY);
+                }
+                float mx[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    mx[i] = __uint_as_float(s[i][0]);
+#pragma unroll
+                    for (int k = 1; k < 31; k += 2) mx[i] = ptx::fmax3(mx[i], __uint_as_float(s[i][k]), __uint_as_float(s[i][k + 1]));
+                    mx[i] = fmaxf(mx[i], __uint_as_float(s[i][31]));
+                }
+                const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+                const bool grows = live && top > m && !((top - m) * c <= kRescaleAt);
+                if (__any_sync(0xffffffffu, grows)) {
+                    const float alpha = grows ? ptx::ex2((m - top) * c) : 1.f;
+                    l *= alpha;
+                    if (grows) m = top;
+                    if (j > 0) {
+                        if (!warp_wait(&sh.pv_done[g], (n - 1) & 1, abort_flag)) return;
+                        ptx::tc_fence_after_sync();
+#pragma unroll 1
+                        for (int i = 0; i < 4; ++i) {
+                            uint32_t o[32];
+                            ptx::tmem_ld_32x32(to + i * 32, o);
+                            ptx::tmem_ld_wait();
+#pragma unroll
+                            for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * alpha);
+                            ptx::tmem_st_32x32(to + i * 32, o);
+                        }
+                    }
+                }
+                const float neg = m == -INFINITY ? 0.f : -m * c;
+                float sum[4] = {0.f, 0.f, 0.f, 0.f};
+                uint32_t pr[64];
+#pragma unroll
+                for (int i = 0; i < 64; ++i) {
+                    const float a = ptx::ex2(fmaf(__uint_as_float(s[i >> 4][(2 * i) & 31]), c, neg));
+                    const float b = ptx::ex2(fmaf(__uint_as_float(s[i >> 4][(2 * i + 1) & 31]), c, neg));
+                    sum[i & 3] += a + b;
+                    const __nv_bfloat162 ab = __floats2bfloat162_rn(a, b);
+                    pr[i] = *reinterpret_cast<const uint32_t*>(&ab);
+                }
+                l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                ptx::tmem_st_32x32(ts, pr);
+                ptx::tmem_st_32x32(ts + 32, pr + 32);
+                ptx::tmem_st_wait();
+                ptx::tc_fence_before_sync();
+            }
+            if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&sh.p_full[g]));
+            __syncwarp();
+        }
+        // ---- the item's outputs ----
+        if (nt > 0 && !warp_wait(&sh.pv_done[g], (n - 1) & 1, abort_flag)) return;
+        ptx::tc_fence_after_sync();
+        if (!it.pair && g == 1) {                // stream 0 adds both up
+            if (!warp_wait(&sh.merge_free, (n_merges & 1) ^ 1, abort_flag)) return;
+            sh.merge_m[row] = m;
+            sh.merge_l[row] = l;
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&sh.merge_full));
+            ++n_merges;
+            ++n_items;
+            continue;
+        }
+        float scale0 = 1.f, scale1 = 0.f, total = l, top = m;
+        if (!it.pair) {
+            if (!warp_wait(&sh.merge_full, n_merges & 1, abort_flag)) return;
+            ++n_merges;
+            const float m1 = sh.merge_m[row], l1 = sh.merge_l[row];
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&sh.merge_free));
+            if (it.nt1 > 0) {
+                top = fmaxf(m, m1);
+                scale0 = m == top ? 1.f : ptx::ex2((m - top) * c);
+                scale1 = m1 == top ? 1.f : ptx::ex2((m1 - top) * c);
+                total = l * scale0 + l1 * scale1;
+            }
+        }
+        const bool two = !it.pair && it.nt1 > 0;
+        const float inv = 1.f / total;
+        scale0 *= inv;
+        scale1 *= inv;
+        const float lse2 = (top == -INFINITY ? 0.f : top * c) + ptx::lg2(total);         // log2
+        const bool nothing = it.partial && total == 0.f;         // a range of which the row sees none
+        const bool odd = sh.odd_values[n_items % kFlags] == (int)n_items + 1;
+        const long long out_row = (long long)(it.q_begin + tok) * p.pages.n_q_heads + q_head;
+        if (any_live) {
+#pragma unroll 1
+            for (int i = 0; i < 4; ++i) {
+                uint32_t o[32];
+                if (nt > 0) {
+                    ptx::tmem_ld_32x32(to + i * 32, o);
+                    ptx::tmem_ld_wait();
+                }
+#pragma unroll
+                for (int k = 0; k < 32; ++k) o[k] = nothing || nt == 0 ? 0u : __float_as_uint(__uint_as_float(o[k]) * scale0);
+                if (two) {
+                    uint32_t o1[32];
+                    ptx::tmem_ld_32x32(to + kHeadDim + i * 32, o1);
+                    ptx::tmem_ld_wait();
+#pragma unroll
+                    for (int k = 0; k < 32; ++k)
+                        if (!nothing) o[k] = __float_as_uint(fmaf(__uint_as_float(o1[k]), scale1, __uint_as_float(o[k])));
+                }
+                if (odd && live) {               // infinities and NaN among the values that this row sees and others don't
+                    for (int t = max(it.min_seen, it.t0 * kTile); t < min(seen, (it.t0 + it.nt) * kTile); ++t) {
+                        const int page = p.pages.page_of(it.index, t, p.status);
+                        if (page < 0) continue;
+                        const uint32_t* v = reinterpret_cast<const uint32_t*>(static_cast<const char*>(p.cache_v) +
+                                                                              2 * (p.pages.row_at(page, t, it.head) + i * 32));
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) {
+                            const uint32_t x = v[k];
+                            if (odd_bf16(x)) o[2 * k] = __float_as_uint(__uint_as_float(o[2 * k]) + __uint_as_float(x << 16));
+                            if (odd_bf16(x >> 16)) o[2 * k + 1] = __float_as_uint(__uint_as_float(o[2 * k + 1]) + __uint_as_float(x & 0xffff0000u));
+                        }
+                    }
+                }
+                if (live && it.partial) {
+                    float4* dst = reinterpret_cast<float4*>(p.part_out + part_row * kHeadDim + i * 32);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        dst[k] = make_float4(__uint_as_float(o[4 * k]), __uint_as_float(o[4 * k + 1]), __uint_as_float(o[4 * k + 2]),
+                                             __uint_as_float(o[4 * k + 3]));
+                } else if (live) {
+                    uint4* dst = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.out) + out_row * kHeadDim + i * 32);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) {
+                            const __nv_bfloat162 ab = __floats2bfloat162_rn(__uint_as_float(o[8 * k + 2 * x]), __uint_as_float(o[8 * k + 2 * x + 1]));
+                            w[x] = *reinterpret_cast<const uint32_t*>(&ab);
+                        }
+                        dst[k] = make_uint4(w[0], w[1], w[2], w[3]);
+                    }
+                }
+                __syncwarp();                    // (tensor memory is read by whole warps)
+            }
+            if (live) {
+                if (it.partial) p.part_lse[part_row] = lse2;
+                else if (p.lse) p.lse[(long long)q_head * p.n_tokens + it.q_begin + tok] = lse2 * 0.6931471805599453f;
+            }
+        }
+        ptx::tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) {
+            if (nt > 0) ptx::mbar_arrive(ptx::smem_u32(&sh.o_free[g]));
+            if (two) ptx::mbar_arrive(ptx::smem_u32(&sh.o_free[1]));
+        }
+        __syncwarp();
+        ++n_items;
+    }
+}
+
+template <int kRequests, bool kStep>
+__global__ void __launch_bounds__(kThreads, 1)
+chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+             const __grid_constant__ ChunkParams p, const __grid_constant__ Batch<ChunkReq, kRequests> batch) {
+    extern __shared__ uint8_t smem_raw[];
+    ChunkShared& sh = *reinterpret_cast<ChunkShared*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+    const int warp = threadIdx.x >> 5;
+    if (threadIdx.x == 0) {
+        const auto init = [](unsigned long long* bar, int count) { ptx::mbar_init(ptx::smem_u32(bar), count); };
+        for (int i = 0; i < 2; ++i) {
+            init(&sh.q_full[i], 1);
+            init(&sh.q_empty[i], 1);
+            init(&sh.s_full[i], 1);
+            init(&sh.p_full[i], 4);
+            init(&sh.pv_done[i], 1);
+            init(&sh.o_free[i], 4);
+        }
+        for (int i = 0; i < kRing; ++i) {
+            init(&sh.full[i], 2);
+            init(&sh.empty[i], 1);
+            init(&sh.dirty[i], 1);
+        }
+        init(&sh.merge_full, 4);
+        init(&sh.merge_free, 4);
+        init(&sh.mma_done, 1);
+        for (int i = 0; i < kFlags; ++i) sh.odd_values[i] = 0;
+        sh.abort_flag = 0;
+        ptx::fence_mbar_init();
+    }
+    if (warp == kMmaWarp) {
+        ptx::tmem_alloc(ptx::smem_u32(&sh.tmem_base), 512);
+        ptx::tmem_relinquish();
+    }
+    ptx::tc_fence_before_sync();
+    __syncthreads();
+    ptx::tc_fence_after_sync();
+    grid_dependency_wait();
+    const uint32_t tmem = sh.tmem_base;
+    if (warp < kSoftmaxWarps) {
+        ptx::more_registers<kSoftmaxRegs>();
+        softmax_rows<kRequests, kStep>(p, batch, sh, tmem);
+    } else {
+        ptx::fewer_registers<kOtherRegs>();
+        if (warp == kLoadWarp) {
+            load_tiles(map_q, map_k, map_v, p, batch, sh);
+        } else if (warp == kMmaWarp) {
+            if ((threadIdx.x & 31) == 0) issue_mmas(p, batch, sh, tmem);
+            __syncwarp();
+        } else {
+            clean_values(p, batch, sh);
+        }
+    }
+    ptx::tc_fence_before_sync();
+    __syncthreads();
+    if (warp == kMmaWarp) {
+        ptx::tc_fence_after_sync();
+        ptx::tmem_dealloc(tmem, 512);
+    }
+    if (threadIdx.x == 0 && sh.abort_flag) atomicMax(p.status, (int)LOOKM_ERR_DEVICE_TIMEOUT);
+}
+
+// ---- ranges added up, weights accumulated -----------------------------------------------------------
+constexpr int kFinishThreads = 256, kFinishWarps = kFinishThreads / 32;
+
+// A warp per output row: the ranges' rows in range order, each times 2^(its log-sum-exp - the row's).
+__device__ __forceinline__ void add_ranges(const ChunkParams& p, const ChunkReq& rq, long long row) {
+    const int lane = threadIdx.x & 31;
+    const long long rows = (long long)rq.n_new * p.pages.n_q_heads;
+    const float* part_lse = p.part_lse + rq.part_begin + row;
+    float top = -INFINITY;
+    for (int s = lane; s < rq.splits; s += 32) top = fmaxf(top, part_lse[s * rows]);
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+    const float ref = top == -INFINITY ? 0.f : top;
+    float total = 0.f;
+    float4 acc = {0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < rq.splits; ++s) {
+        const float x = part_lse[s * rows];
+        if (x == -INFINITY) continue;
+        const float w = ptx::ex2(x - ref);
+        const float4 o = *reinterpret_cast<const float4*>(p.part_out + (rq.part_begin + s * rows + row) * kHeadDim + lane * 4);
+        total += w;
+        acc.x = fmaf(o.x, w, acc.x);
+        acc.y = fmaf(o.y, w, acc.y);
+        acc.z = fmaf(o.z, w, acc.z);
+        acc.w = fmaf(o.w, w, acc.w);
+    }
+    const float inv = 1.f / total;
+    const __nv_bfloat162 lo = __floats2bfloat162_rn(acc.x * inv, acc.y * inv), hi = __floats2bfloat162_rn(acc.z * inv, acc.w * inv);
+    const long long tok = row / p.pages.n_q_heads, head = row - tok * p.pages.n_q_heads;
+    uint2 w;
+    w.x = *reinterpret_cast<const uint32_t*>(&lo);
+    w.y = *reinterpret_cast<const uint32_t*>(&hi);
+    *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.out) + ((rq.q_begin + tok) * p.pages.n_q_heads + head) * kHeadDim + lane * 4) = w;
+    if (lane == 0 && p.lse) p.lse[head * p.n_tokens + rq.q_begin + tok] = (ref + ptx::lg2(total)) * 0.6931471805599453f;
+}
+
+template <int kRequests>
+__global__ void __launch_bounds__(kFinishThreads)
+chunk_finish_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__ Batch<ChunkReq, kRequests> batch) {
+    const ChunkReq& rq = batch.r[blockIdx.y];
+    grid_dependency_wait();
+    if (rq.splits <= 1) return;
+    const long long rows = (long long)rq.n_new * p.pages.n_q_heads;
+    for (long long row = (long long)blockIdx.x * kFinishWarps + (threadIdx.x >> 5); row < rows; row += (long long)gridDim.x * kFinishWarps)
+        add_ranges(p, rq, row);
+}
+
+// Steps: every row's weight, summed over the heads of the group, added to its mass.  blockIdx.x: KV head and block of rows.
+constexpr int kMassRows = 2 * kFinishThreads;
+template <int kRequests>
+__global__ void __launch_bounds__(kFinishThreads)
+step_mass_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__ Batch<ChunkReq, kRequests> batch) {
+    __shared__ float lse2[kTile];
+    const ChunkReq& rq = batch.r[blockIdx.y];
+    const int head = blockIdx.x % p.pages.n_kv_heads, block = blockIdx.x / p.pages.n_kv_heads;
+    if ((long long)block * kMassRows >= rq.len) return;
+    grid_dependency_wait();
+    for (int g = threadIdx.x; g < p.group; g += kFinishThreads)
+        lse2[g] = p.lse[(long long)(head * p.group + g) * p.n_tokens + rq.q_begin] * 1.4426950408889634f;
+    __syncthreads();
+    for (int t = block * kMassRows + threadIdx.x; t < min(rq.len, (block + 1) * kMassRows); t += kFinishThreads) {
+        const int page = p.pages.page_of(rq.index, t, p.status);
+        const float* logits = p.logits + rq.logits_begin + (long long)head * p.group * rq.len + t;
+        float w = 0.f;
+        for (int g = 0; g < p.group; ++g) w += ptx::ex2(fmaf(logits[(long long)g * rq.len], p.scale_log2, -lse2[g]));
+        if (page >= 0) p.mass[p.pages.mass_at(page, t, head)] += w;
+    }
+}
+
+template <int kRequests>
+Batch<ChunkReq, kRequests> shorter(const Batch<ChunkReq, kManyRequests>& batch) {
+    Batch<ChunkReq, kRequests> b;
+    b.n = batch.n;
+    b.pad = 0;
+    for (int i = 0; i < kRequests; ++i) b.r[i] = i < batch.n ? batch.r[i] : ChunkReq{0, 0, 0, 0, 0, 0, 1, 0, 0, 0};
+    return b;
+}
+
+template <int kRequests, bool kStep>
+cudaError_t launch(const CUtensorMap& map_q, const CUtensorMap& map_k, const CUtensorMap& map_v, const ChunkParams& p,
+                   const Batch<ChunkReq, kManyRequests>& batch, int grid, cudaStream_t stream) {
+    constexpr size_t smem = sizeof(ChunkShared) + 1024;
+    static unsigned long long configured = 0;
+    cudaError_t err = once_per_device(configured, [] {
+        return cudaFuncSetAttribute(chunk_kernel<kRequests, kStep>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    });
+    if (err != cudaSuccess) return err;
+    return launch_chained(chunk_kernel<kRequests, kStep>, dim3(grid), dim3(kThreads), smem, stream, map_q, map_k, map_v, p,
+                          shorter<kRequests>(batch));
+}
+
+template <int kRequests>
+cudaError_t finish(const ChunkParams& p, const Batch<ChunkReq, kManyRequests>& batch, cudaStream_t stream, bool mass) {
+    long long rows = 0, len = 0;
+    for (int i = 0; i < batch.n; ++i) {
+        if (batch.r[i].splits > 1) rows = std::max(rows, (long long)batch.r[i].n_new * p.pages.n_q_heads);
+        len = std::max<long long>(len, batch.r[i].len);
+    }
+    if (mass)
+        return launch_chained(step_mass_kernel<kRequests>, dim3((unsigned)((len + kMassRows - 1) / kMassRows * p.pages.n_kv_heads), batch.n),
+                              dim3(kFinishThreads), 0, stream, p, shorter<kRequests>(batch));
+    return launch_chained(chunk_finish_kernel<kRequests>, dim3((unsigned)std::min<long long>((rows + kFinishWarps - 1) / kFinishWarps, 4096), batch.n),
+                          dim3(kFinishThreads), 0, stream, p, shorter<kRequests>(batch));
+}
+
+}  // namespace
+
+cudaError_t launch_chunk(const CUtensorMap& map_q, const CUtensorMap& map_k, const CUtensorMap& map_v, const ChunkParams& p,
+                         const Batch<ChunkReq, kManyRequests>& batch, int grid, cudaStream_t stream) {
+    const bool few = batch.n <= kFewRequests;
+    if (p.logits)
+        return few ? launch<kFewRequests, true>(map_q, map_k, map_v, p, batch, grid, stream)
+                   : launch<kManyRequests, true>(map_q, map_k, map_v, p, batch, grid, stream);
+    return few ? launch<kFewRequests, false>(map_q, map_k, map_v, p, batch, grid, stream)
+               : launch<kManyRequests, false>(map_q, map_k, map_v, p, batch, grid, stream);
+}
+
+cudaError_t launch_chunk_ranges(const ChunkParams& p, const Batch<ChunkReq, kManyRequests>& batch, cudaStream_t stream) {
+    return batch.n <= kFewRequests ? finish<kFewRequests>(p, batch, stream, false) : finish<kManyRequests>(p, batch, stream, false);
+}
+cudaError_t launch_step_mass(const ChunkParams& p, const Batch<ChunkReq, kManyRequests>& batch, cudaStream_t stream) {
+    return batch.n <= kFewRequests ? finish<kFewRequests>(p, batch, stream, true) : finish<kManyRequests>(p, batch, stream, true);
+}
+
+}  // namespace lookm

@@ -66,6 +66,42 @@ struct AppendParams {
 };
 cudaError_t launch_append(const AppendParams& p, const Batch<AppendReq, kManyRequests>& batch, int num_sms, cudaStream_t stream);
 
+// ---- chunk_kernel.cu -----------------------------------------------------------------------------
+// Attention of the newest tokens of each request.  The query rows of a KV head are (token, query head of the group) pairs, the
+// heads of a token side by side; a tile has the rows of kTile / group tokens.
+struct ChunkReq {
+    int q_begin, n_new;          // its tokens on the packed axis
+    int len;                     // cached rows, the new ones included
+    int index;                   // of the request in the page table
+    int item_begin;              // first work item
+    int n_sets;                  // two query tiles each, the last perhaps one
+    int splits;                  // ranges that the cached rows are cut into
+    int pad;
+    long long part_begin;        // splits > 1: first partial row, in rows: [split][token][query head]
+    long long logits_begin;      // steps: first logit of its [query head][row] block
+};
+struct ChunkParams {
+    Pages pages;
+    int group, tile_tokens;      // query heads of a KV head, tokens of a query tile
+    int n_items;
+    int n_tokens;                // on the packed axis (= the row stride of lse)
+    float scale_log2;            // softmax scale * log2(e)
+    const void* cache_v;
+    void* out;                   // [tokens, n_q_heads, 128] bf16
+    float* lse;                  // [n_q_heads, tokens] or NULL
+    float* part_out;             // partial rows, normalised: [row][128]
+    float* part_lse;             // their log2-sum-exp2
+    float* logits;               // steps: q.k of every row (unscaled)
+    float* mass;                 // steps
+    int* status;
+};
+cudaError_t launch_chunk(const CUtensorMap& map_q, const CUtensorMap& map_k, const CUtensorMap& map_v, const ChunkParams& p,
+                         const Batch<ChunkReq, kManyRequests>& batch, int grid, cudaStream_t stream);
+// Adds up the ranges of requests that have several.
+cudaError_t launch_chunk_ranges(const ChunkParams& p, const Batch<ChunkReq, kManyRequests>& batch, cudaStream_t stream);
+// Steps: adds every row's weight to its mass.
+cudaError_t launch_step_mass(const ChunkParams& p, const Batch<ChunkReq, kManyRequests>& batch, cudaStream_t stream);
+
 // ---- evict_kernels.cu ------------------------------------------------------------------------------
 struct EvictReq {
     int len, budget, window;     // window <= budget <= len

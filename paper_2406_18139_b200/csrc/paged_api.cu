@@ -3,6 +3,7 @@
 #include <algorithm>
 #include <cmath>
 #include <initializer_list>
+#include <vector>
 
 #include "host.h"
 #include "paged.h"
@@ -208,6 +209,209 @@ int evict(const void* cache_k, const void* cache_v, const float* mass, const int
     return LOOKM_OK;
 }
 
+// ---- attention of the newest tokens -----------------------------------------------------------------
+constexpr int kMaxRanges = 64;           // of the cached rows of an item
+constexpr int kMinRangeTiles = 2;        // tiles of cached rows in a range, at least
+constexpr int kMaxRangeItems = 640;      // items of a call that has ranges
+
+struct ChunkPlan {
+    std::vector<ChunkReq> reqs;          // longest items first
+    int tile_tokens = 1;
+    bool ranges = false;
+    size_t o_parts, o_part_lse, o_logits, o_lse, total;
+};
+
+// Tiles of cached rows that the item of a request's last set streams, and its work: tiles times query tiles.
+struct Longest { int tiles, steps; };
+Longest longest_item(const ChunkReq& q, int tile_tokens) {
+    const int tiles = (q.len + kTile - 1) / kTile, last = (q.n_new + tile_tokens - 1) / tile_tokens;
+    return {tiles, last > 1 ? 2 * tiles : tiles};
+}
+
+size_t part_rows_bound(const lookm_paged_layout* l, int n, const int* new_lens, const int* lens) {
+    size_t rows = 0;
+    for (int r = 0; r < n; ++r) {
+        const size_t ranges = std::min<size_t>(kMaxRanges, ((size_t)lens[r] + kMinRangeTiles * kTile - 1) / (kMinRangeTiles * kTile));
+        rows += (new_lens ? (size_t)std::max(new_lens[r], 1) : 1) * l->n_q_heads * ranges;
+    }
+    return std::min<size_t>(rows, (size_t)kMaxRangeItems * 2 * kTile);
+}
+
+size_t chunk_workspace(size_t part_rows, size_t logits, size_t lse, ChunkPlan* pl) {
+    size_t o = kStatusBytes;
+    auto carve = [&](size_t bytes) { size_t at = o; o = align_up(o + bytes, 256); return at; };
+    const size_t parts = carve(4 * part_rows * kHeadDim), part_lse = carve(4 * part_rows), lo = carve(4 * logits), ls = carve(4 * lse);
+    if (pl) {
+        pl->o_parts = parts;
+        pl->o_part_lse = part_lse;
+        pl->o_logits = lo;
+        pl->o_lse = ls;
+        pl->total = o;
+    }
+    return o;
+}
+
+// How the rows are cut.  Enough items for the SMs: not at all.  Else into ranges, so that all items together are one wave,
+// or, where the items alone are more than a wave, none is longer than half of what an SM has to do.
+void plan_ranges(ChunkPlan& pl, const lookm_paged_layout* l, int sms) {
+    long long items = 0, steps = 0;
+    for (const ChunkReq& q : pl.reqs) {
+        const Longest it = longest_item(q, pl.tile_tokens);
+        items += (long long)l->n_kv_heads * q.n_sets;
+        steps += (long long)l->n_kv_heads * q.n_sets * it.steps;
+    }
+    if (items == 0 || items >= kMaxRangeItems / 2) return;
+    const auto ranges = [&](const ChunkReq& q, long long limit) {
+        const Longest it = longest_item(q, pl.tile_tokens);
+        const long long most = std::min<long long>(kMaxRanges, (it.tiles + kMinRangeTiles - 1) / kMinRangeTiles);
+        return (int)std::max<long long>(1, std::min<long long>(most, (it.steps + limit - 1) / limit));
+    };
+    const auto count = [&](long long limit) {
+        long long n = 0;
+        for (const ChunkReq& q : pl.reqs) n += (long long)l->n_kv_heads * q.n_sets * ranges(q, limit);
+        return n;
+    };
+    long long limit = std::max<long long>(1, steps / sms);
+    if (items <= sms) {
+        long long lo = limit, hi = 2ll * ((1ll << 30) / kTile + 1);
+        while (lo < hi) {
+            const long long mid = lo + (hi - lo) / 2;
+            if (count(mid) > sms) lo = mid + 1; else hi = mid;
+        }
+        limit = lo;
+    } else {
+        limit = std::max<long long>(1, limit / 2);
+        while (count(limit) > kMaxRangeItems) limit *= 2;
+    }
+    for (ChunkReq& q : pl.reqs) {
+        q.splits = ranges(q, limit);
+        pl.ranges = pl.ranges || q.splits > 1;
+    }
+}
+
+// bf16 [tokens, heads, 128]: boxes of the rows of a query tile
+int make_map_q(CUtensorMap* map, const void* base, long long tokens, const lookm_paged_layout* l, int group, int tile_tokens) {
+    auto enc = tensor_map_encoder();
+    if (!enc) return LOOKM_ERR_CUDA;
+    cuuint64_t dims[3] = {(cuuint64_t)kHeadDim, (cuuint64_t)l->n_q_heads, (cuuint64_t)tokens};
+    cuuint64_t strides[2] = {(cuuint64_t)l->q_stride_head * 2, (cuuint64_t)l->q_stride_tok * 2};
+    cuuint32_t box[3] = {64, (cuuint32_t)group, (cuuint32_t)tile_tokens};
+    cuuint32_t estr[3] = {1, 1, 1};
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
+               ? LOOKM_OK : LOOKM_ERR_CUDA;
+}
+// A pool: boxes of (a part of) a page of one head
+int make_map_pool(CUtensorMap* map, const void* base, const lookm_paged_layout* l) {
+    auto enc = tensor_map_encoder();
+    if (!enc) return LOOKM_ERR_CUDA;
+    cuuint64_t dims[4] = {(cuuint64_t)kHeadDim, (cuuint64_t)l->page_rows, (cuuint64_t)l->n_kv_heads, (cuuint64_t)l->n_pages};
+    cuuint64_t strides[3] = {(cuuint64_t)l->row_stride * 2, (cuuint64_t)l->head_stride * 2, (cuuint64_t)l->page_stride * 2};
+    cuuint32_t box[4] = {64, (cuuint32_t)std::min(l->page_rows, kTile), 1, 1};
+    cuuint32_t estr[4] = {1, 1, 1, 1};
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
+               ? LOOKM_OK : LOOKM_ERR_CUDA;
+}
+
+// cu: NULL for a step (one token per request, weights accumulated into mass).
+int chunk_attention(const void* q, const void* cache_k, const void* cache_v, float* mass, const int* table, const int* cu, const int* lens,
+                    int n, const lookm_paged_layout* paged, void* out, float* lse, void* ws, size_t ws_bytes, void* stream) {
+    LOOKM_TRY(check_paged(paged));
+    const bool step = cu == nullptr;
+    if (!q || !out || !aligned(q, 16) || !aligned(out, 16) || !aligned(lse, 4)) return LOOKM_ERR_INVALID_ARG;
+    if (step && (!mass || !aligned(mass, 4))) return LOOKM_ERR_INVALID_ARG;
+    for (long long s : {paged->q_stride_tok, paged->q_stride_head}) {
+        if (s <= 0 || s % 8) return LOOKM_ERR_INVALID_ARG;
+        if (s >= (1ll << 38)) return LOOKM_ERR_UNSUPPORTED;
+    }
+    if (!step) LOOKM_TRY(check_tokens(n, cu));
+    LOOKM_TRY(check_requests(paged, n, lens));
+    LOOKM_TRY(check_pool(cache_k, cache_v, table));
+    const int group = paged->n_q_heads / paged->n_kv_heads;
+    const long long tokens = step ? n : cu[n];
+    ChunkPlan pl;
+    pl.tile_tokens = kTile / group;
+    long long logits = 0, part_rows = 0, max_items = 0;
+    for (int r = 0; r < n; ++r) {
+        ChunkReq c;
+        c.q_begin = step ? r : cu[r];
+        c.n_new = step ? 1 : cu[r + 1] - cu[r];
+        c.len = lens[r];
+        c.index = r;
+        c.item_begin = 0;
+        c.n_sets = ((c.n_new + pl.tile_tokens - 1) / pl.tile_tokens + 1) / 2;
+        c.splits = 1;
+        c.pad = 0;
+        c.part_begin = 0;
+        c.logits_begin = logits;
+        if (c.len < c.n_new) return LOOKM_ERR_INVALID_ARG;
+        logits += step ? (long long)c.len * paged->n_q_heads : 0;
+        if (c.n_new) pl.reqs.push_back(c);
+        max_items += (long long)c.n_sets * paged->n_kv_heads;
+    }
+    if (max_items + kMaxRangeItems >= (1ll << 31) || tokens * paged->n_q_heads >= (1ll << 40)) return LOOKM_ERR_UNSUPPORTED;
+    DeviceInfo di;
+    const int known = device_info(di);           // (asked again below: the plan needs no device)
+    plan_ranges(pl, paged, known == LOOKM_OK && di.sms > 0 ? di.sms : 148);
+    for (ChunkReq& c : pl.reqs) {
+        c.part_begin = part_rows;
+        if (c.splits > 1) part_rows += (long long)c.splits * c.n_new * paged->n_q_heads;
+    }
+    chunk_workspace(part_rows, logits, step && !lse ? tokens * paged->n_q_heads : 0, &pl);
+    LOOKM_TRY(check_ws(ws, ws_bytes, pl.total));
+    LOOKM_TRY(known);
+    g_launches = 0;
+    if (pl.reqs.empty()) return LOOKM_OK;
+    std::stable_sort(pl.reqs.begin(), pl.reqs.end(), [&](const ChunkReq& a, const ChunkReq& b) {
+        return (long long)longest_item(a, pl.tile_tokens).steps * b.splits > (long long)longest_item(b, pl.tile_tokens).steps * a.splits;
+    });
+    CUtensorMap map_q, map_k, map_v;
+    LOOKM_TRY(make_map_q(&map_q, q, tokens, paged, group, pl.tile_tokens));
+    LOOKM_TRY(make_map_pool(&map_k, cache_k, paged));
+    LOOKM_TRY(make_map_pool(&map_v, cache_v, paged));
+    ChunkParams p;
+    p.pages = pages_of(paged, table);
+    p.group = group;
+    p.tile_tokens = pl.tile_tokens;
+    p.n_tokens = (int)tokens;
+    p.scale_log2 = (paged->softmax_scale > 0.f ? paged->softmax_scale : 1.0f / std::sqrt((float)kHeadDim)) * 1.4426950408889634f;
+    p.cache_v = cache_v;
+    p.out = out;
+    p.lse = lse ? lse : step ? at<float>(ws, pl.o_lse) : nullptr;
+    p.part_out = at<float>(ws, pl.o_parts);
+    p.part_lse = at<float>(ws, pl.o_part_lse);
+    p.logits = step ? at<float>(ws, pl.o_logits) : nullptr;
+    p.mass = mass;
+    p.status = at<int>(ws, 0);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    for (size_t base = 0; base < pl.reqs.size(); base += kManyRequests) {
+        Batch<ChunkReq, kManyRequests> b;
+        b.n = (int)std::min<size_t>(kManyRequests, pl.reqs.size() - base);
+        b.pad = 0;
+        long long items = 0;
+        bool ranges = false;
+        for (int i = 0; i < b.n; ++i) {
+            b.r[i] = pl.reqs[base + i];
+            b.r[i].item_begin = (int)items;
+            items += (long long)b.r[i].n_sets * b.r[i].splits * paged->n_kv_heads;
+            ranges = ranges || b.r[i].splits > 1;
+        }
+        p.n_items = (int)items;
+        LOOKM_CUDA(launch_chunk(map_q, map_k, map_v, p, b, (int)std::min<long long>(items, di.sms), st));
+        ++g_launches;
+        if (ranges) {
+            LOOKM_CUDA(launch_chunk_ranges(p, b, st));
+            ++g_launches;
+        }
+        if (step) {
+            LOOKM_CUDA(launch_step_mass(p, b, st));
+            ++g_launches;
+        }
+    }
+    return LOOKM_OK;
+}
+
 }  // namespace
 }  // namespace lookm
 
@@ -218,10 +422,15 @@ extern "C" {
 size_t lookm_paged_workspace_size(const lookm_paged_layout* paged, int n_requests, const int* new_lens_host,
                                   const int* cache_lens_host) {
     if (check_paged(paged) != LOOKM_OK || check_requests(paged, n_requests, cache_lens_host) != LOOKM_OK) return 0;
-    size_t rows = 0;
-    for (int r = 0; r < n_requests; ++r) rows += cache_lens_host[r];
-    (void)new_lens_host;
-    return align_up(kStatusBytes + 4 * rows * paged->n_kv_heads, 256);
+    size_t rows = 0, tokens = 0;
+    for (int r = 0; r < n_requests; ++r) {
+        if (new_lens_host && new_lens_host[r] < 0) return 0;
+        rows += cache_lens_host[r];
+        tokens += new_lens_host ? new_lens_host[r] : 1;
+    }
+    const size_t attention = chunk_workspace(part_rows_bound(paged, n_requests, new_lens_host, cache_lens_host), rows * paged->n_q_heads,
+                                             std::max(tokens, (size_t)n_requests) * paged->n_q_heads, nullptr);
+    return std::max(align_up(kStatusBytes + 4 * rows * paged->n_kv_heads, 256), attention);
 }
 
 int lookm_append_rows(const void* q, const void* k, const void* v, const int* positions, const int* cu_seqlens_host,
@@ -231,6 +440,25 @@ int lookm_append_rows(const void* q, const void* k, const void* v, const int* po
     return guarded([&] {
         return append_rows(q, k, v, positions, cu_seqlens_host, cache_lens_host, n_requests, layout, options, q_out, cache_k, cache_v, mass,
                            page_table, paged, workspace, workspace_bytes, cuda_stream);
+    });
+}
+
+int lookm_chunk_attention(const void* q, const void* cache_k, const void* cache_v, const int* page_table, const int* cu_seqlens_host,
+                          const int* cache_lens_host, int n_requests, const lookm_paged_layout* paged, void* out, float* lse,
+                          void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    if (!cu_seqlens_host) return LOOKM_ERR_INVALID_ARG;
+    return guarded([&] {
+        return chunk_attention(q, cache_k, cache_v, nullptr, page_table, cu_seqlens_host, cache_lens_host, n_requests, paged, out, lse,
+                               workspace, workspace_bytes, cuda_stream);
+    });
+}
+
+int lookm_step_attention(const void* q, const void* cache_k, const void* cache_v, float* mass, const int* page_table,
+                         const int* cache_lens_host, int n_requests, const lookm_paged_layout* paged, void* out, float* lse,
+                         void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    return guarded([&] {
+        return chunk_attention(q, cache_k, cache_v, mass, page_table, nullptr, cache_lens_host, n_requests, paged, out, lse, workspace,
+                               workspace_bytes, cuda_stream);
     });
 }
 
