@@ -40,17 +40,17 @@ constexpr float kRescaleAt = 8.f;                // log2 of the growth of a row'
 struct __align__(1024) ChunkShared {
     uint8_t q[2][kTileBytes];
     uint8_t ring[kRing][kTileBytes];
-    float merge_m[kTile], merge_l[kTile];        // one query tile: stream 1's reference and sum
     unsigned long long q_full[2], q_empty[2];
     unsigned long long full[kRing], empty[kRing];
     unsigned long long dirty[kRing];             // V tiles that warps 10 and 11 have to look at; they make them full
-    unsigned long long s_full[2], p_full[2], pv_done[2], o_free[2];
+    unsigned long long s_full[2], p_half[2], p_full[2], pv_done[2], o_free[2];
     unsigned long long merge_full, merge_free, mma_done;
+    float merge_m[kTile], merge_l[kTile];        // one query tile: stream 1's reference and sum
     int odd_values[kFlags];                      // V had infinities or NaN that were taken out
     uint32_t tmem_base;
     int abort_flag;
 };
-static_assert(sizeof(ChunkShared) + 1024 <= 232448, "shared memory exceeds 227 KB");
+static_assert(sizeof(ChunkShared) <= 232448, "shared memory exceeds 227 KB");
 
 struct Item {
     int q_begin, n_new, len, index, head, split;
@@ -202,17 +202,21 @@ __device__ __forceinline__ void load_tiles(const CUtensorMap& map_q, const CUten
     __syncwarp();
 }
 
-// ---- warp 9, one thread ---------------------------------------------------------------------------
+// ---- warp 9 ---------------------------------------------------------------------------------------
+// The whole warp walks through the protocol and one lane issues: what the instructions take then lies in uniform registers.  (With
+// one lane alone in the code, the eight MMAs of a product took 670 clocks to issue, more than their 512 to run.)
 template <int kRequests>
 __device__ __forceinline__ void issue_mmas(const ChunkParams& p, const Batch<ChunkReq, kRequests>& batch, ChunkShared& sh, uint32_t tmem) {
     const int rounds = (p.n_items + gridDim.x - 1) / gridDim.x;
     volatile int* abort_flag = &sh.abort_flag;
     constexpr uint32_t idesc_s = ptx::umma_idesc_bf16(kTile, kTile), idesc_o = ptx::umma_idesc_bf16(kTile, kHeadDim) | ptx::kIdescBMnMajor;
     uint32_t n = 0, nq = 0;
-    uint32_t np[2] = {0, 0}, no[2] = {0, 0};     // tiles and items of a stream so far
+    uint32_t p_phase = 0, o_phase = 3;           // a bit per stream: parity of the wait for its next probabilities, for its free outputs
     bool stop = false;
+    const bool leader = ptx::elect_one();
+    const auto commit = [&](unsigned long long* bar) { if (leader) ptx::umma_commit(ptx::smem_u32(bar)); };
     const auto wait = [&](unsigned long long* bar, uint32_t parity) {
-        if (!stop && !ptx::mbar_wait(ptx::smem_u32(bar), parity, abort_flag)) stop = true;
+        if (!stop && !warp_wait(bar, parity, abort_flag)) stop = true;
     };
     for (int round = 0; round < rounds && !stop; ++round) {
         const int item = item_of_round(round, p.n_items);
@@ -223,27 +227,39 @@ __device__ __forceinline__ void issue_mmas(const ChunkParams& p, const Batch<Chu
         for (int g = 0; g < tiles; ++g) wait(&sh.q_full[(nq + g) & 1], ((nq + g) >> 1) & 1);
         const auto qk = [&](int g, uint32_t stage) {             // S of stream g = its query tile x K^T
             if (stop) return;
-            const uint32_t a = ptx::smem_u32(&sh.q[(nq + (it.pair ? g : 0)) & 1][0]), b = ptx::smem_u32(&sh.ring[stage][0]);
+            const uint64_t a = ptx::umma_desc_sw128(ptx::smem_u32(&sh.q[(nq + (it.pair ? g : 0)) & 1][0])),
+                           b = ptx::umma_desc_sw128(ptx::smem_u32(&sh.ring[stage][0]));
+            const uint32_t d = tmem + g * kTile;
+            if (leader) {
 #pragma unroll
-            for (int kk = 0; kk < 8; ++kk) {
-                const uint32_t off = (kk >> 2) * kHalfBytes + (kk & 3) * 32;
-                ptx::umma_bf16(tmem + g * kTile, ptx::umma_desc_sw128(a + off), ptx::umma_desc_sw128(b + off), idesc_s, kk > 0);
+                for (int kk = 0; kk < 8; ++kk) {             // (descriptors count in units of 16 bytes)
+                    const uint32_t off = ((kk >> 2) * kHalfBytes + (kk & 3) * 32) >> 4;
+                    ptx::umma_bf16(d, a + off, b + off, idesc_s, kk > 0);
+                }
             }
-            ptx::umma_commit(ptx::smem_u32(&sh.s_full[g]));
+            commit(&sh.s_full[g]);
         };
-        bool fresh[2] = {true, true};            // the stream's output block has nothing of this item yet
+        uint32_t begun = 0;                      // a bit per stream: its output block has something of this item
         const auto pv = [&](int g, uint32_t stage) {             // O of stream g += P x V
-            wait(&sh.p_full[g], np[g] & 1);
+            wait(&sh.p_half[g], (p_phase >> g) & 1);
             if (stop) return;
-            ++np[g];
             ptx::tc_fence_after_sync();
-            const uint32_t b = ptx::smem_u32(&sh.ring[stage][0]);
+            const uint64_t b = ptx::umma_desc_sw128_mn(ptx::smem_u32(&sh.ring[stage][0]), kHalfBytes);
+            const uint32_t d = tmem + 2 * kTile + g * kHeadDim, pr = tmem + g * kTile, more = begun >> g & 1;
+            if (leader) {
 #pragma unroll
-            for (int kk = 0; kk < 8; ++kk)
-                ptx::umma_bf16_ts(tmem + 2 * kTile + g * kHeadDim, tmem + g * kTile + kk * 8,
-                                  ptx::umma_desc_sw128_mn(b + kk * 2048, kHalfBytes), idesc_o, kk > 0 || !fresh[g]);
-            fresh[g] = false;
-            ptx::umma_commit(ptx::smem_u32(&sh.pv_done[g]));
+                for (int kk = 0; kk < 4; ++kk) ptx::umma_bf16_ts(d, pr + kk * 8, b + kk * (2048 >> 4), idesc_o, kk > 0 ? 1u : more);
+            }
+            wait(&sh.p_full[g], (p_phase >> g) & 1);
+            if (stop) return;
+            ptx::tc_fence_after_sync();
+            if (leader) {
+#pragma unroll
+                for (int kk = 4; kk < 8; ++kk) ptx::umma_bf16_ts(d, pr + kk * 8, b + kk * (2048 >> 4), idesc_o, 1u);
+            }
+            p_phase ^= 1u << g;
+            begun |= 1u << g;
+            commit(&sh.pv_done[g]);
         };
         const auto arrived = [&] {               // the next tile of the ring
             const uint32_t s = n % kRing;
@@ -252,14 +268,14 @@ __device__ __forceinline__ void issue_mmas(const ChunkParams& p, const Batch<Chu
             if (!stop) ptx::tc_fence_after_sync();
             return s;
         };
-        const auto release = [&](uint32_t s) { if (!stop) ptx::umma_commit(ptx::smem_u32(&sh.empty[s])); };
+        const auto release = [&](uint32_t s) { if (!stop) commit(&sh.empty[s]); };
         const auto queries_done = [&] {
-            for (int g = 0; g < tiles && !stop; ++g) ptx::umma_commit(ptx::smem_u32(&sh.q_empty[(nq + g) & 1]));
+            for (int g = 0; g < tiles && !stop; ++g) commit(&sh.q_empty[(nq + g) & 1]);
         };
         // the output blocks are free when the epilogue of the item before has read them
         const auto outputs_free = [&] {
-            if (it.nt0 > 0) wait(&sh.o_free[0], (no[0]++ & 1) ^ 1);
-            if (it.nt1 > 0) wait(&sh.o_free[1], (no[1]++ & 1) ^ 1);
+            if (it.nt0 > 0) { wait(&sh.o_free[0], o_phase & 1); o_phase ^= 1; }
+            if (it.nt1 > 0) { wait(&sh.o_free[1], o_phase >> 1); o_phase ^= 2; }
         };
         if (it.pair) {
             uint32_t k = arrived();
@@ -306,8 +322,9 @@ __device__ __forceinline__ void issue_mmas(const ChunkParams& p, const Batch<Chu
         nq += tiles;
     }
     int ignore = 0;                              // no MMA may be running when TMEM is released
-    ptx::umma_commit(ptx::smem_u32(&sh.mma_done));
+    commit(&sh.mma_done);
     ptx::mbar_wait(ptx::smem_u32(&sh.mma_done), 0, &ignore, 1000000000ull);
+    __syncwarp();
 }
 
 // ---- warps 10 and 11 --------------------------------------------------------------------------------
@@ -355,6 +372,22 @@ __device__ __forceinline__ void clean_values(const ChunkParams& p, const Batch<C
 }
 
 // ---- warps 0 to 7 ------------------------------------------------------------------------------------
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+    const __nv_bfloat162 ab = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&ab);
+}
+
+// 32 logits of a row as probabilities 2^(s * c + neg), in bf16 pairs; adds them up (before the rounding).
+__device__ __forceinline__ void probabilities(const uint32_t (&s)[32], ptx::f32x2 c, ptx::f32x2 neg, ptx::f32x2 (&sum)[4], uint32_t (&pr)[16]) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const float2 x = ptx::unpack2(ptx::fma2(ptx::pack2(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), c, neg));
+        const float a = ptx::ex2(x.x), b = ptx::ex2(x.y);
+        sum[i & 3] = ptx::add2(sum[i & 3], ptx::pack2(a, b));
+        pr[i] = pack_bf16(a, b);
+    }
+}
+
 template <int kRequests, bool kStep>
 __device__ __forceinline__ void softmax_rows(const ChunkParams& p, const Batch<ChunkReq, kRequests>& batch, ChunkShared& sh, uint32_t tmem) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = warp >> 2, row = (warp & 3) * 32 + lane;
@@ -368,39 +401,47 @@ __device__ __forceinline__ void softmax_rows(const ChunkParams& p, const Batch<C
     for (int round = 0; round < rounds; ++round) {
         const int item = item_of_round(round, p.n_items);
         if (item < 0) continue;
-        const Item it = decode_item(p, batch, item);
-        const int tok = it.tok0 + (it.pair ? g * p.tile_tokens : 0) + tok_in_tile;
-        const bool live = tok_in_tile < p.tile_tokens && tok < it.n_new;
-        const bool any_live = __any_sync(0xffffffffu, live);
-        const int seen = live ? it.len - it.n_new + tok + 1 : 0x7fffffff;
-        const int nt = g ? it.nt1 : it.nt0;
-        const int q_head = it.head * p.group + head_in_group;
-        const long long part_row = it.part_begin + ((long long)it.split * it.n_new + tok) * p.pages.n_q_heads + q_head;
-        if (it.nt == 0) {                        // a range of nothing: no role does anything for it
-            if (live && (it.pair || g == 0)) p.part_lse[part_row] = -INFINITY;
-            continue;
+        int seen, t_first, t_step, nt;           // rows that the thread's row sees; the stream's tiles
+        bool live, any_live;                     // whether the row has a token, and any of the warp's has one
+        float* to_logits = nullptr;
+        {
+            const Item it = decode_item(p, batch, item);
+            const int tok = it.tok0 + (it.pair ? g * p.tile_tokens : 0) + tok_in_tile;
+            live = tok_in_tile < p.tile_tokens && tok < it.n_new;
+            any_live = __any_sync(0xffffffffu, live);
+            seen = live ? it.len - it.n_new + tok + 1 : 0x7fffffff;
+            nt = g ? it.nt1 : it.nt0;
+            t_first = it.t0 + (it.pair ? 0 : g);
+            t_step = it.pair ? 1 : 2;
+            const int q_head = it.head * p.group + head_in_group;
+            if (it.nt == 0) {                    // a range of nothing: no role does anything for it
+                if (live && (it.pair || g == 0))
+                    p.part_lse[it.part_begin + ((long long)it.split * it.n_new + tok) * p.pages.n_q_heads + q_head] = -INFINITY;
+                continue;
+            }
+            if constexpr (kStep) to_logits = p.logits + it.logits_begin + (long long)q_head * it.len;
         }
-        float m = -INFINITY, l = 0.f;
+        float m = -INFINITY, l = 0.f;            // reference, sum
         for (int j = 0; j < nt; ++j, ++n) {
-            const int t = it.t0 + (it.pair ? j : 2 * j + g);
+            const int t = t_first + j * t_step;
             if (!warp_wait(&sh.s_full[g], n & 1, abort_flag)) return;
             if (any_live) {
-                ptx::tc_fence_after_sync();
                 uint32_t s[4][32];
+                ptx::tc_fence_after_sync();
 #pragma unroll
                 for (int i = 0; i < 4; ++i) ptx::tmem_ld_32x32(ts + i * 32, s[i]);
+                const int cols = seen - t * kTile;
+                const bool masked = __any_sync(0xffffffffu, cols < kTile);
                 ptx::tmem_ld_wait();
                 if constexpr (kStep) {
-                    if (live) {
-                        float* to_logits = p.logits + it.logits_begin + (long long)(it.head * p.group + head_in_group) * it.len + t * kTile;
-                        const int cols = min(kTile, it.len - t * kTile);
+                    if (live) {                  // (a step's rows see all that is cached)
 #pragma unroll
                         for (int i = 0; i < kTile; ++i)
-                            if (i < cols) to_logits[i] = __uint_as_float(s[i >> 5][i & 31]);
+                            if (i < cols) to_logits[t * kTile + i] = __uint_as_float(s[i >> 5][i & 31]);
                     }
+                    __syncwarp();
                 }
-                const int cols = seen - t * kTile;
-                if (__any_sync(0xffffffffu, cols < kTile)) {
+                if (masked) {
 #pragma unroll
                     for (int i = 0; i < kTile; ++i)
                         if (i >= cols) s[i >> 5][i & 31] = __float_as_uint(-INFINITY);
@@ -423,37 +464,46 @@ __device__ __forceinline__ void softmax_rows(const ChunkParams& p, const Batch<C
                         if (!warp_wait(&sh.pv_done[g], (n - 1) & 1, abort_flag)) return;
                         ptx::tc_fence_after_sync();
 #pragma unroll 1
-                        for (int i = 0; i < 4; ++i) {
-                            uint32_t o[32];
-                            ptx::tmem_ld_32x32(to + i * 32, o);
+                        for (int i = 0; i < kHeadDim; i += 16) {
+                            uint32_t o[16];
+                            ptx::tmem_ld_32x16(to + i, o);
                             ptx::tmem_ld_wait();
 #pragma unroll
-                            for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * alpha);
-                            ptx::tmem_st_32x32(to + i * 32, o);
+                            for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * alpha);
+                            ptx::tmem_st_32x16(to + i, o);
                         }
                     }
                 }
-                const float neg = m == -INFINITY ? 0.f : -m * c;
-                float sum[4] = {0.f, 0.f, 0.f, 0.f};
-                uint32_t pr[64];
+                const float neg1 = m == -INFINITY ? 0.f : -m * c;
+                const ptx::f32x2 c2 = ptx::pack2(c, c), neg = ptx::pack2(neg1, neg1);
+                ptx::f32x2 sum[4] = {0, 0, 0, 0};
+                uint32_t pr[16];
 #pragma unroll
-                for (int i = 0; i < 64; ++i) {
-                    const float a = ptx::ex2(fmaf(__uint_as_float(s[i >> 4][(2 * i) & 31]), c, neg));
-                    const float b = ptx::ex2(fmaf(__uint_as_float(s[i >> 4][(2 * i + 1) & 31]), c, neg));
-                    sum[i & 3] += a + b;
-                    const __nv_bfloat162 ab = __floats2bfloat162_rn(a, b);
-                    pr[i] = *reinterpret_cast<const uint32_t*>(&ab);
+                for (int h = 0; h < 2; ++h) {    // the product with V begins with the first half of the rows
+#pragma unroll
+                    for (int i = 2 * h; i < 2 * h + 2; ++i) {
+                        probabilities(s[i], c2, neg, sum, pr);
+                        ptx::tmem_st_32x16(ts + i * 16, pr);
+                    }
+                    ptx::tmem_st_wait();
+                    ptx::tc_fence_before_sync();
+                    if (h == 0 && lane == 0) ptx::mbar_arrive(ptx::smem_u32(&sh.p_half[g]));
+                    __syncwarp();
                 }
-                l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-                ptx::tmem_st_32x32(ts, pr);
-                ptx::tmem_st_32x32(ts + 32, pr + 32);
-                ptx::tmem_st_wait();
-                ptx::tc_fence_before_sync();
+                const float2 v = ptx::unpack2(ptx::add2(ptx::add2(sum[0], sum[1]), ptx::add2(sum[2], sum[3])));
+                l += v.x + v.y;
+            } else if (lane == 0) {
+                ptx::mbar_arrive(ptx::smem_u32(&sh.p_half[g]));
             }
             if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&sh.p_full[g]));
             __syncwarp();
         }
         // ---- the item's outputs ----
+        int again = item;                        // (decoded again: the tiles' loop has no registers for what is only needed here)
+        asm volatile("" : "+r"(again));
+        const Item it = decode_item(p, batch, again);
+        const int tok = it.tok0 + (it.pair ? g * p.tile_tokens : 0) + tok_in_tile, q_head = it.head * p.group + head_in_group;
+        const long long part_row = it.part_begin + ((long long)it.split * it.n_new + tok) * p.pages.n_q_heads + q_head;
         if (nt > 0 && !warp_wait(&sh.pv_done[g], (n - 1) & 1, abort_flag)) return;
         ptx::tc_fence_after_sync();
         if (!it.pair && g == 1) {                // stream 0 adds both up
@@ -490,30 +540,30 @@ __device__ __forceinline__ void softmax_rows(const ChunkParams& p, const Batch<C
         const long long out_row = (long long)(it.q_begin + tok) * p.pages.n_q_heads + q_head;
         if (any_live) {
 #pragma unroll 1
-            for (int i = 0; i < 4; ++i) {
-                uint32_t o[32];
+            for (int i = 0; i < kHeadDim; i += 16) {
+                uint32_t o[16];
                 if (nt > 0) {
-                    ptx::tmem_ld_32x32(to + i * 32, o);
+                    ptx::tmem_ld_32x16(to + i, o);
                     ptx::tmem_ld_wait();
                 }
 #pragma unroll
-                for (int k = 0; k < 32; ++k) o[k] = nothing || nt == 0 ? 0u : __float_as_uint(__uint_as_float(o[k]) * scale0);
+                for (int k = 0; k < 16; ++k) o[k] = nothing || nt == 0 ? 0u : __float_as_uint(__uint_as_float(o[k]) * scale0);
                 if (two) {
-                    uint32_t o1[32];
-                    ptx::tmem_ld_32x32(to + kHeadDim + i * 32, o1);
+                    uint32_t o1[16];
+                    ptx::tmem_ld_32x16(to + kHeadDim + i, o1);
                     ptx::tmem_ld_wait();
 #pragma unroll
-                    for (int k = 0; k < 32; ++k)
+                    for (int k = 0; k < 16; ++k)
                         if (!nothing) o[k] = __float_as_uint(fmaf(__uint_as_float(o1[k]), scale1, __uint_as_float(o[k])));
                 }
                 if (odd && live) {               // infinities and NaN among the values that this row sees and others don't
                     for (int t = max(it.min_seen, it.t0 * kTile); t < min(seen, (it.t0 + it.nt) * kTile); ++t) {
                         const int page = p.pages.page_of(it.index, t, p.status);
                         if (page < 0) continue;
-                        const uint32_t* v = reinterpret_cast<const uint32_t*>(static_cast<const char*>(p.cache_v) +
-                                                                              2 * (p.pages.row_at(page, t, it.head) + i * 32));
+                        const uint32_t* v =
+                            reinterpret_cast<const uint32_t*>(static_cast<const char*>(p.cache_v) + 2 * (p.pages.row_at(page, t, it.head) + i));
 #pragma unroll
-                        for (int k = 0; k < 16; ++k) {
+                        for (int k = 0; k < 8; ++k) {
                             const uint32_t x = v[k];
                             if (odd_bf16(x)) o[2 * k] = __float_as_uint(__uint_as_float(o[2 * k]) + __uint_as_float(x << 16));
                             if (odd_bf16(x >> 16)) o[2 * k + 1] = __float_as_uint(__uint_as_float(o[2 * k + 1]) + __uint_as_float(x & 0xffff0000u));
@@ -521,21 +571,16 @@ __device__ __forceinline__ void softmax_rows(const ChunkParams& p, const Batch<C
                     }
                 }
                 if (live && it.partial) {
-                    float4* dst = reinterpret_cast<float4*>(p.part_out + part_row * kHeadDim + i * 32);
+                    uint4* dst = reinterpret_cast<uint4*>(p.part_out + part_row * kHeadDim + i);
 #pragma unroll
-                    for (int k = 0; k < 8; ++k)
-                        dst[k] = make_float4(__uint_as_float(o[4 * k]), __uint_as_float(o[4 * k + 1]), __uint_as_float(o[4 * k + 2]),
-                                             __uint_as_float(o[4 * k + 3]));
+                    for (int k = 0; k < 4; ++k) dst[k] = make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
                 } else if (live) {
-                    uint4* dst = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.out) + out_row * kHeadDim + i * 32);
+                    uint4* dst = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.out) + out_row * kHeadDim + i);
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
+                    for (int k = 0; k < 2; ++k) {
                         uint32_t w[4];
 #pragma unroll
-                        for (int x = 0; x < 4; ++x) {
-                            const __nv_bfloat162 ab = __floats2bfloat162_rn(__uint_as_float(o[8 * k + 2 * x]), __uint_as_float(o[8 * k + 2 * x + 1]));
-                            w[x] = *reinterpret_cast<const uint32_t*>(&ab);
-                        }
+                        for (int x = 0; x < 4; ++x) w[x] = pack_bf16(__uint_as_float(o[8 * k + 2 * x]), __uint_as_float(o[8 * k + 2 * x + 1]));
                         dst[k] = make_uint4(w[0], w[1], w[2], w[3]);
                     }
                 }
@@ -561,8 +606,12 @@ template <int kRequests, bool kStep>
 __global__ void __launch_bounds__(kThreads, 1)
 chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
              const __grid_constant__ ChunkParams p, const __grid_constant__ Batch<ChunkReq, kRequests> batch) {
-    extern __shared__ uint8_t smem_raw[];
-    ChunkShared& sh = *reinterpret_cast<ChunkShared*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    ChunkShared& sh = *reinterpret_cast<ChunkShared*>(smem_raw);
+    if (ptx::smem_u32(smem_raw) & 1023u) {       // (the swizzle needs it, and there is no room to round up in)
+        if (threadIdx.x == 0) atomicMax(p.status, (int)LOOKM_ERR_UNSUPPORTED);
+        return;
+    }
     const int warp = threadIdx.x >> 5;
     if (threadIdx.x == 0) {
         const auto init = [](unsigned long long* bar, int count) { ptx::mbar_init(ptx::smem_u32(bar), count); };
@@ -570,6 +619,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
             init(&sh.q_full[i], 1);
             init(&sh.q_empty[i], 1);
             init(&sh.s_full[i], 1);
+            init(&sh.p_half[i], 4);
             init(&sh.p_full[i], 4);
             init(&sh.pv_done[i], 1);
             init(&sh.o_free[i], 4);
@@ -603,8 +653,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
         if (warp == kLoadWarp) {
             load_tiles(map_q, map_k, map_v, p, batch, sh);
         } else if (warp == kMmaWarp) {
-            if ((threadIdx.x & 31) == 0) issue_mmas(p, batch, sh, tmem);
-            __syncwarp();
+            issue_mmas(p, batch, sh, tmem);
         } else {
             clean_values(p, batch, sh);
         }
@@ -699,7 +748,7 @@ Batch<ChunkReq, kRequests> shorter(const Batch<ChunkReq, kManyRequests>& batch) 
 template <int kRequests, bool kStep>
 cudaError_t launch(const CUtensorMap& map_q, const CUtensorMap& map_k, const CUtensorMap& map_v, const ChunkParams& p,
                    const Batch<ChunkReq, kManyRequests>& batch, int grid, cudaStream_t stream) {
-    constexpr size_t smem = sizeof(ChunkShared) + 1024;
+    constexpr size_t smem = sizeof(ChunkShared);
     static unsigned long long configured = 0;
     cudaError_t err = once_per_device(configured, [] {
         return cudaFuncSetAttribute(chunk_kernel<kRequests, kStep>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
