@@ -53,59 +53,112 @@ struct __align__(1024) ChunkShared {
 static_assert(sizeof(ChunkShared) <= 232448, "shared memory exceeds 227 KB");
 
 struct Item {
-    int q_begin, n_new, len, index, head, split;
+    int q_begin, n_new, len, index, head;
     int tok0;                                    // of its first query tile
     bool pair;                                   // two query tiles
-    bool partial;                                // a range of the rows
+    bool partial;                                // a piece of a unit
+    int piece;
     int t0;                                      // first tile of cached rows
-    int nt, nt0, nt1;                            // tiles of cached rows: all (loaded), of stream 0, of stream 1
+    int nt, nt0, nt1;                            // tiles of cached rows: all (loaded; at least one), of stream 0, of stream 1
     int min_seen;                                // cached rows that its first token sees: every row of the item sees these
-    long long part_begin, logits_begin;
+    long long logits_begin;
 };
 
-template <int kRequests>
-__device__ __forceinline__ Item decode_item(const ChunkParams& p, const Batch<ChunkReq, kRequests>& batch, int item) {
-    int lo = 0, hi = batch.n - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (batch.r[mid].item_begin <= item) lo = mid; else hi = mid - 1;
+// The items of a CTA, which every role walks through by itself.  Either whole units, those of the longest requests and of
+// these the sets that see most first, dealt in serpentine order; or equal shares of all units' steps, in which a
+// CTA's first and last item may be a piece of a unit.
+struct Walk {
+    int round;
+    int pos, begin;                              // shares: position, first step of the unit that it is in
+    int r, head, set;                            // that unit
+
+    template <int kRequests>
+    __device__ __forceinline__ void start(const ChunkParams& p, const Batch<ChunkReq, kRequests>& batch) {
+        round = 0;
+        if (p.share == 0) return;
+        pos = blockIdx.x * p.share;
+        int lo = 0, hi = batch.n - 1;
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (batch.r[mid].step_begin <= pos) lo = mid; else hi = mid - 1;
+        }
+        r = lo;
+        const ChunkReq& q = batch.r[r];
+        head = (pos - q.step_begin) / q.head_steps;
+        begin = q.step_begin + head * q.head_steps;
+        set = 0;
+        for (;;) {
+            const int n = chunk_unit(q, set, p.tile_tokens).steps;
+            if (begin + n > pos || set + 1 == q.n_sets) break;
+            begin += n;
+            ++set;
+        }
     }
-    const ChunkReq& rq = batch.r[lo];
-    int u = item - rq.item_begin;
-    Item it;
-    it.head = u % p.pages.n_kv_heads;
-    u /= p.pages.n_kv_heads;
-    it.split = u % rq.splits;
-    const int set = rq.n_sets - 1 - u / rq.splits;           // those that see most rows first
-    it.q_begin = rq.q_begin;
-    it.n_new = rq.n_new;
-    it.len = rq.len;
-    it.index = rq.index;
-    it.tok0 = set * 2 * p.tile_tokens;
-    it.pair = it.tok0 + p.tile_tokens < rq.n_new;
-    it.partial = rq.splits > 1;
-    it.part_begin = rq.part_begin;
-    it.logits_begin = rq.logits_begin;
-    const int before = rq.len - rq.n_new;
-    it.min_seen = before + it.tok0 + 1;
-    const int seen0 = before + min(rq.n_new, it.tok0 + p.tile_tokens), seen1 = before + min(rq.n_new, it.tok0 + 2 * p.tile_tokens);
-    const int tiles0 = (seen0 + kTile - 1) / kTile, tiles = it.pair ? (seen1 + kTile - 1) / kTile : tiles0;
-    it.t0 = (int)((long long)tiles * it.split / rq.splits);
-    it.nt = (int)((long long)tiles * (it.split + 1) / rq.splits) - it.t0;
-    if (it.pair) {
-        it.nt1 = it.nt;
-        it.nt0 = min(max(tiles0 - it.t0, 0), it.nt);
-    } else {
-        it.nt0 = (it.nt + 1) >> 1;
-        it.nt1 = it.nt >> 1;
+    // False: there is no further item.
+    template <int kRequests>
+    __device__ __forceinline__ bool next(const ChunkParams& p, const Batch<ChunkReq, kRequests>& batch, Item& it) {
+        ChunkUnit u;
+        int t0, t1, at_r;
+        if (p.share == 0) {
+            const int n = gridDim.x, i = round * n + ((round & 1) ? n - 1 - (int)blockIdx.x : (int)blockIdx.x);
+            if (round * n >= p.n_units) return false;
+            ++round;
+            if (i >= p.n_units) return false;    // (only the last round is not full)
+            int lo = 0, hi = batch.n - 1;
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) >> 1;
+                if (batch.r[mid].unit_begin <= i) lo = mid; else hi = mid - 1;
+            }
+            at_r = lo;
+            const int k = i - batch.r[lo].unit_begin;
+            it.head = k % p.pages.n_kv_heads;
+            u = chunk_unit(batch.r[lo], batch.r[lo].n_sets - 1 - k / p.pages.n_kv_heads, p.tile_tokens);
+            t0 = 0;
+            t1 = u.tiles;
+            it.piece = 0;
+        } else {
+            const int first = blockIdx.x * p.share, end = min(first + p.share, p.total_steps);
+            do {
+                if (pos >= end) return false;
+                at_r = r;
+                it.head = head;
+                const ChunkReq& q = batch.r[r];
+                u = chunk_unit(q, set, p.tile_tokens);
+                t0 = chunk_cut(u, pos - begin);
+                t1 = chunk_cut(u, end - begin);
+                it.piece = 2 * blockIdx.x + (pos == first ? 0 : 1);
+                pos = begin + u.steps;
+                if (pos <= end) {                // on to the next unit
+                    begin = pos;
+                    if (++set == q.n_sets) {
+                        set = 0;
+                        if (++head == p.pages.n_kv_heads) { head = 0; ++r; }
+                    }
+                }
+            } while (t0 == t1);
+        }
+        const ChunkReq& q = batch.r[at_r];
+        it.q_begin = q.q_begin;
+        it.n_new = q.n_new;
+        it.len = q.len;
+        it.index = q.index;
+        it.logits_begin = q.logits_begin;
+        it.tok0 = u.tok0;
+        it.pair = u.pair;
+        it.min_seen = q.len - q.n_new + u.tok0 + 1;
+        it.t0 = t0;
+        it.nt = t1 - t0;
+        it.partial = it.nt != u.tiles;
+        if (u.pair) {
+            it.nt1 = it.nt;
+            it.nt0 = min(max(u.tiles0 - t0, 0), it.nt);
+        } else {
+            it.nt0 = (it.nt + 1) >> 1;
+            it.nt1 = it.nt >> 1;
+        }
+        return true;
     }
-    return it;
-}
-// Serpentine deal of the items; -1: a round in which this CTA has none
-__device__ __forceinline__ int item_of_round(int round, int n_items) {
-    const int n = gridDim.x, item = round * n + ((round & 1) ? n - 1 - (int)blockIdx.x : (int)blockIdx.x);
-    return item < n_items ? item : -1;
-}
+};
 // Whether some row of the item does not see all 128 rows of tile t (or the cache ends in it).
 __device__ __forceinline__ bool is_masked(const Item& it, int t) { return (it.t0 + t + 1) * kTile > it.min_seen; }
 
@@ -120,7 +173,7 @@ __device__ __forceinline__ bool odd_bf16(uint32_t x) { return (x & 0x7f80u) == 0
 template <int kRequests>
 __device__ __forceinline__ void load_tiles(const CUtensorMap& map_q, const CUtensorMap& map_k, const CUtensorMap& map_v,
                                            const ChunkParams& p, const Batch<ChunkReq, kRequests>& batch, ChunkShared& sh) {
-    const int lane = threadIdx.x & 31, rounds = (p.n_items + gridDim.x - 1) / gridDim.x;
+    const int lane = threadIdx.x & 31;
     volatile int* abort_flag = &sh.abort_flag;
     if (lane == 0) {
         ptx::prefetch_tensormap(&map_q);
@@ -132,11 +185,10 @@ __device__ __forceinline__ void load_tiles(const CUtensorMap& map_q, const CUten
     uint32_t n = 0, nq = 0;                      // tiles and query tiles armed so far
     uint32_t dirty_phase = 0, last_dirty = 0;    // per stage: parity of its next use as a dirty one, whether its last use was one
     bool stop = false;
-    for (int round = 0; round < rounds && !stop; ++round) {
-        const int item = item_of_round(round, p.n_items);
-        if (item < 0) continue;
-        const Item it = decode_item(p, batch, item);
-        if (it.nt == 0) continue;                // (a set that sees fewer tiles than there are ranges)
+    Walk walk;
+    Item it;
+    walk.start(p, batch);
+    while (!stop && walk.next(p, batch, it)) {
         for (int g = 0; g < (it.pair ? 2 : 1) && !stop; ++g, ++nq) {
             const int s = nq & 1;
             if (!warp_wait(&sh.q_empty[s], ((nq >> 1) & 1) ^ 1, abort_flag)) { stop = true; break; }
@@ -207,7 +259,6 @@ __device__ __forceinline__ void load_tiles(const CUtensorMap& map_q, const CUten
 // one lane alone in the code, the eight MMAs of a product took 670 clocks to issue, more than their 512 to run.)
 template <int kRequests>
 __device__ __forceinline__ void issue_mmas(const ChunkParams& p, const Batch<ChunkReq, kRequests>& batch, ChunkShared& sh, uint32_t tmem) {
-    const int rounds = (p.n_items + gridDim.x - 1) / gridDim.x;
     volatile int* abort_flag = &sh.abort_flag;
     constexpr uint32_t idesc_s = ptx::umma_idesc_bf16(kTile, kTile), idesc_o = ptx::umma_idesc_bf16(kTile, kHeadDim) | ptx::kIdescBMnMajor;
     uint32_t n = 0, nq = 0;
@@ -218,11 +269,10 @@ __device__ __forceinline__ void issue_mmas(const ChunkParams& p, const Batch<Chu
     const auto wait = [&](unsigned long long* bar, uint32_t parity) {
         if (!stop && !warp_wait(bar, parity, abort_flag)) stop = true;
     };
-    for (int round = 0; round < rounds && !stop; ++round) {
-        const int item = item_of_round(round, p.n_items);
-        if (item < 0) continue;
-        const Item it = decode_item(p, batch, item);
-        if (it.nt == 0) continue;
+    Walk walk;
+    Item it;
+    walk.start(p, batch);
+    while (!stop && walk.next(p, batch, it)) {
         const int tiles = it.pair ? 2 : 1;
         for (int g = 0; g < tiles; ++g) wait(&sh.q_full[(nq + g) & 1], ((nq + g) >> 1) & 1);
         const auto qk = [&](int g, uint32_t stage) {             // S of stream g = its query tile x K^T
@@ -330,14 +380,13 @@ __device__ __forceinline__ void issue_mmas(const ChunkParams& p, const Batch<Chu
 // ---- warps 10 and 11 --------------------------------------------------------------------------------
 template <int kRequests>
 __device__ __forceinline__ void clean_values(const ChunkParams& p, const Batch<ChunkReq, kRequests>& batch, ChunkShared& sh) {
-    const int lane = threadIdx.x & 31, half = (threadIdx.x >> 5) - kCleanWarp, rounds = (p.n_items + gridDim.x - 1) / gridDim.x;
+    const int lane = threadIdx.x & 31, half = (threadIdx.x >> 5) - kCleanWarp;
     volatile int* abort_flag = &sh.abort_flag;
     uint32_t n = 0, n_items = 0, phase = 0;
-    for (int round = 0; round < rounds; ++round) {
-        const int item = item_of_round(round, p.n_items);
-        if (item < 0) continue;
-        const Item it = decode_item(p, batch, item);
-        if (it.nt == 0) continue;
+    Walk walk;
+    Item it;
+    walk.start(p, batch);
+    while (walk.next(p, batch, it)) {
         for (int t = 0; t < it.nt; ++t) {
             // the ring position of V tile t: K and V take turns, with one K tile ahead, or two with one query tile
             const uint32_t at = n + (it.pair ? 2 * t + 1 : t < it.nt - 1 ? 2 * t + 2 : 2 * t + 1);
@@ -391,36 +440,23 @@ __device__ __forceinline__ void probabilities(const uint32_t (&s)[32], ptx::f32x
 template <int kRequests, bool kStep>
 __device__ __forceinline__ void softmax_rows(const ChunkParams& p, const Batch<ChunkReq, kRequests>& batch, ChunkShared& sh, uint32_t tmem) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = warp >> 2, row = (warp & 3) * 32 + lane;
-    const int rounds = (p.n_items + gridDim.x - 1) / gridDim.x;
     volatile int* abort_flag = &sh.abort_flag;
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint32_t ts = tmem + g * kTile + lanes, to = tmem + 2 * kTile + g * kHeadDim + lanes;
     const float c = p.scale_log2;
     const int tok_in_tile = row / p.group, head_in_group = row - tok_in_tile * p.group;
     uint32_t n = 0, n_items = 0, n_merges = 0;
-    for (int round = 0; round < rounds; ++round) {
-        const int item = item_of_round(round, p.n_items);
-        if (item < 0) continue;
-        int seen, t_first, t_step, nt;           // rows that the thread's row sees; the stream's tiles
-        bool live, any_live;                     // whether the row has a token, and any of the warp's has one
+    Walk walk;
+    Item it;
+    walk.start(p, batch);
+    while (walk.next(p, batch, it)) {
+        const int tok = it.tok0 + (it.pair ? g * p.tile_tokens : 0) + tok_in_tile, q_head = it.head * p.group + head_in_group;
+        const bool live = tok_in_tile < p.tile_tokens && tok < it.n_new;         // the row has a token
+        const bool any_live = __any_sync(0xffffffffu, live);
+        const int seen = live ? it.len - it.n_new + tok + 1 : 0x7fffffff;
+        const int nt = g ? it.nt1 : it.nt0, t_first = it.t0 + (it.pair ? 0 : g), t_step = it.pair ? 1 : 2;
         float* to_logits = nullptr;
-        {
-            const Item it = decode_item(p, batch, item);
-            const int tok = it.tok0 + (it.pair ? g * p.tile_tokens : 0) + tok_in_tile;
-            live = tok_in_tile < p.tile_tokens && tok < it.n_new;
-            any_live = __any_sync(0xffffffffu, live);
-            seen = live ? it.len - it.n_new + tok + 1 : 0x7fffffff;
-            nt = g ? it.nt1 : it.nt0;
-            t_first = it.t0 + (it.pair ? 0 : g);
-            t_step = it.pair ? 1 : 2;
-            const int q_head = it.head * p.group + head_in_group;
-            if (it.nt == 0) {                    // a range of nothing: no role does anything for it
-                if (live && (it.pair || g == 0))
-                    p.part_lse[it.part_begin + ((long long)it.split * it.n_new + tok) * p.pages.n_q_heads + q_head] = -INFINITY;
-                continue;
-            }
-            if constexpr (kStep) to_logits = p.logits + it.logits_begin + (long long)q_head * it.len;
-        }
+        if constexpr (kStep) to_logits = p.logits + it.logits_begin + (long long)q_head * it.len;
         float m = -INFINITY, l = 0.f;            // reference, sum
         for (int j = 0; j < nt; ++j, ++n) {
             const int t = t_first + j * t_step;
@@ -499,11 +535,6 @@ __device__ __forceinline__ void softmax_rows(const ChunkParams& p, const Batch<C
             __syncwarp();
         }
         // ---- the item's outputs ----
-        int again = item;                        // (decoded again: the tiles' loop has no registers for what is only needed here)
-        asm volatile("" : "+r"(again));
-        const Item it = decode_item(p, batch, again);
-        const int tok = it.tok0 + (it.pair ? g * p.tile_tokens : 0) + tok_in_tile, q_head = it.head * p.group + head_in_group;
-        const long long part_row = it.part_begin + ((long long)it.split * it.n_new + tok) * p.pages.n_q_heads + q_head;
         if (nt > 0 && !warp_wait(&sh.pv_done[g], (n - 1) & 1, abort_flag)) return;
         ptx::tc_fence_after_sync();
         if (!it.pair && g == 1) {                // stream 0 adds both up
@@ -537,6 +568,7 @@ __device__ __forceinline__ void softmax_rows(const ChunkParams& p, const Batch<C
         const float lse2 = (top == -INFINITY ? 0.f : top * c) + ptx::lg2(total);         // log2
         const bool nothing = it.partial && total == 0.f;         // a range of which the row sees none
         const bool odd = sh.odd_values[n_items % kFlags] == (int)n_items + 1;
+        const long long part_row = (long long)it.piece * p.slot_rows + (tok - it.tok0) * p.group + head_in_group;
         const long long out_row = (long long)(it.q_begin + tok) * p.pages.n_q_heads + q_head;
         if (any_live) {
 #pragma unroll 1
@@ -667,72 +699,122 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
     if (threadIdx.x == 0 && sh.abort_flag) atomicMax(p.status, (int)LOOKM_ERR_DEVICE_TIMEOUT);
 }
 
-// ---- ranges added up, weights accumulated -----------------------------------------------------------
+// ---- pieces added up, weights accumulated -----------------------------------------------------------
 constexpr int kFinishThreads = 256, kFinishWarps = kFinishThreads / 32;
+constexpr int kMassRows = 2 * kFinishThreads;    // cached rows of a CTA
 
-// A warp per output row: the ranges' rows in range order, each times 2^(its log-sum-exp - the row's).
-__device__ __forceinline__ void add_ranges(const ChunkParams& p, const ChunkReq& rq, long long row) {
+// What a unit was cut into: CTAs first .. last, some of which may have none of its tiles.
+struct Cuts {
+    ChunkUnit u;
+    int begin, first, last, pieces;
+    __device__ __forceinline__ Cuts(const ChunkParams& p, const ChunkReq& q, int head, int set) {
+        first = last = 0;
+        pieces = 1;
+        u = chunk_unit(q, set, p.tile_tokens);
+        if (p.share == 0) return;
+        begin = q.step_begin + head * q.head_steps;
+        for (int s = 0; s < set; ++s) begin += chunk_unit(q, s, p.tile_tokens).steps;
+        first = begin / p.share;
+        last = (begin + u.steps - 1) / p.share;
+        pieces = 0;
+        for (int c = first; c <= last; ++c) pieces += piece_of(p, c) >= 0;
+    }
+    // The piece that CTA c has; -1: none
+    __device__ __forceinline__ int piece_of(const ChunkParams& p, int c) const {
+        const int from = c * p.share - begin, to = from + p.share;
+        if (chunk_cut(u, max(from, 0)) == chunk_cut(u, to)) return -1;
+        return 2 * c + (from >= 0 ? 0 : c == first ? 1 : 0);
+    }
+};
+
+// log2-sum-exp2 of a row of a unit that was cut; by a whole warp.
+__device__ __forceinline__ float row_lse2(const ChunkParams& p, const Cuts& cuts, int row, float& top) {
     const int lane = threadIdx.x & 31;
-    const long long rows = (long long)rq.n_new * p.pages.n_q_heads;
-    const float* part_lse = p.part_lse + rq.part_begin + row;
-    float top = -INFINITY;
-    for (int s = lane; s < rq.splits; s += 32) top = fmaxf(top, part_lse[s * rows]);
+    top = -INFINITY;
+    for (int c = cuts.first + lane; c <= cuts.last; c += 32) {
+        const int piece = cuts.piece_of(p, c);
+        if (piece >= 0) top = fmaxf(top, p.part_lse[(long long)piece * p.slot_rows + row]);
+    }
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-    const float ref = top == -INFINITY ? 0.f : top;
-    float total = 0.f;
-    float4 acc = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < rq.splits; ++s) {
-        const float x = part_lse[s * rows];
-        if (x == -INFINITY) continue;
-        const float w = ptx::ex2(x - ref);
-        const float4 o = *reinterpret_cast<const float4*>(p.part_out + (rq.part_begin + s * rows + row) * kHeadDim + lane * 4);
-        total += w;
-        acc.x = fmaf(o.x, w, acc.x);
-        acc.y = fmaf(o.y, w, acc.y);
-        acc.z = fmaf(o.z, w, acc.z);
-        acc.w = fmaf(o.w, w, acc.w);
+    if (top == -INFINITY) top = 0.f;
+    float sum = 0.f;
+    for (int c = cuts.first + lane; c <= cuts.last; c += 32) {
+        const int piece = cuts.piece_of(p, c);
+        if (piece >= 0) sum += ptx::ex2(p.part_lse[(long long)piece * p.slot_rows + row] - top);
     }
-    const float inv = 1.f / total;
-    const __nv_bfloat162 lo = __floats2bfloat162_rn(acc.x * inv, acc.y * inv), hi = __floats2bfloat162_rn(acc.z * inv, acc.w * inv);
-    const long long tok = row / p.pages.n_q_heads, head = row - tok * p.pages.n_q_heads;
-    uint2 w;
-    w.x = *reinterpret_cast<const uint32_t*>(&lo);
-    w.y = *reinterpret_cast<const uint32_t*>(&hi);
-    *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.out) + ((rq.q_begin + tok) * p.pages.n_q_heads + head) * kHeadDim + lane * 4) = w;
-    if (lane == 0 && p.lse) p.lse[head * p.n_tokens + rq.q_begin + tok] = (ref + ptx::lg2(total)) * 0.6931471805599453f;
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    return top + ptx::lg2(sum);
 }
 
-template <int kRequests>
+// An output row of a unit that was cut, by a whole warp: the pieces' rows in order, each times 2^(its log-sum-exp - the row's).
+__device__ __forceinline__ void add_pieces(const ChunkParams& p, const ChunkReq& q, const Cuts& cuts, int head, int row) {
+    const int lane = threadIdx.x & 31;
+    float top;
+    const float lse2 = row_lse2(p, cuts, row, top);
+    float4 acc = {0.f, 0.f, 0.f, 0.f};
+    for (int c0 = cuts.first; c0 <= cuts.last; c0 += 32) {
+        const int mine = c0 + lane <= cuts.last ? cuts.piece_of(p, c0 + lane) : -1;
+        const float x = mine >= 0 ? p.part_lse[(long long)mine * p.slot_rows + row] : -INFINITY;
+        const float w = x == -INFINITY ? 0.f : ptx::ex2(x - lse2);
+        const int n = min(32, cuts.last - c0 + 1);
+#pragma unroll 8
+        for (int i = 0; i < n; ++i) {
+            const int piece = __shfl_sync(0xffffffffu, mine, i);
+            const float wi = __shfl_sync(0xffffffffu, w, i), xi = __shfl_sync(0xffffffffu, x, i);
+            if (xi == -INFINITY) continue;
+            const float4 o = *reinterpret_cast<const float4*>(p.part_out + ((long long)piece * p.slot_rows + row) * kHeadDim + lane * 4);
+            acc.x = fmaf(o.x, wi, acc.x);
+            acc.y = fmaf(o.y, wi, acc.y);
+            acc.z = fmaf(o.z, wi, acc.z);
+            acc.w = fmaf(o.w, wi, acc.w);
+        }
+    }
+    const long long tok = q.q_begin + cuts.u.tok0 + row / p.group;
+    const int q_head = head * p.group + row % p.group;
+    const float none = lse2 == -INFINITY ? NAN : 0.f;          // no row has a weight
+    *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.out) + (tok * p.pages.n_q_heads + q_head) * kHeadDim + lane * 4) =
+        make_uint2(pack_bf16(acc.x + none, acc.y + none), pack_bf16(acc.z + none, acc.w + none));
+    if (lane == 0 && p.lse) p.lse[(long long)q_head * p.n_tokens + tok] = lse2 * 0.6931471805599453f;
+}
+
+// blockIdx.x: unit; blockIdx.y: its rows in turn, or with weights blocks of cached rows (of which the first also has the rows).
+template <int kRequests, bool kStep>
 __global__ void __launch_bounds__(kFinishThreads)
 chunk_finish_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__ Batch<ChunkReq, kRequests> batch) {
-    const ChunkReq& rq = batch.r[blockIdx.y];
-    grid_dependency_wait();
-    if (rq.splits <= 1) return;
-    const long long rows = (long long)rq.n_new * p.pages.n_q_heads;
-    for (long long row = (long long)blockIdx.x * kFinishWarps + (threadIdx.x >> 5); row < rows; row += (long long)gridDim.x * kFinishWarps)
-        add_ranges(p, rq, row);
-}
-
-// Steps: every row's weight, summed over the heads of the group, added to its mass.  blockIdx.x: KV head and block of rows.
-constexpr int kMassRows = 2 * kFinishThreads;
-template <int kRequests>
-__global__ void __launch_bounds__(kFinishThreads)
-step_mass_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__ Batch<ChunkReq, kRequests> batch) {
     __shared__ float lse2[kTile];
-    const ChunkReq& rq = batch.r[blockIdx.y];
-    const int head = blockIdx.x % p.pages.n_kv_heads, block = blockIdx.x / p.pages.n_kv_heads;
-    if ((long long)block * kMassRows >= rq.len) return;
-    grid_dependency_wait();
-    for (int g = threadIdx.x; g < p.group; g += kFinishThreads)
-        lse2[g] = p.lse[(long long)(head * p.group + g) * p.n_tokens + rq.q_begin] * 1.4426950408889634f;
-    __syncthreads();
-    for (int t = block * kMassRows + threadIdx.x; t < min(rq.len, (block + 1) * kMassRows); t += kFinishThreads) {
-        const int page = p.pages.page_of(rq.index, t, p.status);
-        const float* logits = p.logits + rq.logits_begin + (long long)head * p.group * rq.len + t;
-        float w = 0.f;
-        for (int g = 0; g < p.group; ++g) w += ptx::ex2(fmaf(logits[(long long)g * rq.len], p.scale_log2, -lse2[g]));
-        if (page >= 0) p.mass[p.pages.mass_at(page, t, head)] += w;
+    int lo = 0, hi = batch.n - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (batch.r[mid].unit_begin <= (int)blockIdx.x) lo = mid; else hi = mid - 1;
+    }
+    const ChunkReq& q = batch.r[lo];
+    const int k = blockIdx.x - q.unit_begin, head = k % p.pages.n_kv_heads, warp = threadIdx.x >> 5;
+    const Cuts cuts(p, q, head, k / p.pages.n_kv_heads);
+    grid_dependency_wait();                      // (also by CTAs that leave: this grid's end has to mean the end of the one before it)
+    if (kStep ? (long long)blockIdx.y * kMassRows >= q.len : cuts.pieces == 1) return;
+    if (cuts.pieces > 1) {
+        const int rows = min(q.n_new - cuts.u.tok0, 2 * p.tile_tokens) * p.group;
+        if (!kStep || blockIdx.y == 0)
+            for (int row = (kStep ? 0 : blockIdx.y * kFinishWarps) + warp; row < rows; row += (kStep ? 1 : gridDim.y) * kFinishWarps)
+                add_pieces(p, q, cuts, head, row);
+    }
+    if constexpr (kStep) {
+        for (int g = warp; g < p.group; g += kFinishWarps) {
+            float top;
+            const float x = cuts.pieces > 1 ? row_lse2(p, cuts, g, top)
+                                            : p.lse[(long long)(head * p.group + g) * p.n_tokens + q.q_begin] * 1.4426950408889634f;
+            if ((threadIdx.x & 31) == 0) lse2[g] = x;
+        }
+        __syncthreads();
+        for (int t = blockIdx.y * kMassRows + threadIdx.x; t < min(q.len, ((int)blockIdx.y + 1) * kMassRows); t += kFinishThreads) {
+            const int page = p.pages.page_of(q.index, t, p.status);
+            const float* logits = p.logits + q.logits_begin + (long long)head * p.group * q.len + t;
+            float w = 0.f;
+            for (int g = 0; g < p.group; ++g) w += ptx::ex2(fmaf(logits[(long long)g * q.len], p.scale_log2, -lse2[g]));
+            if (page >= 0) p.mass[p.pages.mass_at(page, t, head)] += w;
+        }
     }
 }
 
@@ -741,7 +823,7 @@ Batch<ChunkReq, kRequests> shorter(const Batch<ChunkReq, kManyRequests>& batch) 
     Batch<ChunkReq, kRequests> b;
     b.n = batch.n;
     b.pad = 0;
-    for (int i = 0; i < kRequests; ++i) b.r[i] = i < batch.n ? batch.r[i] : ChunkReq{0, 0, 0, 0, 0, 0, 1, 0, 0, 0};
+    for (int i = 0; i < kRequests; ++i) b.r[i] = i < batch.n ? batch.r[i] : ChunkReq{0, 0, 0, 0, 0, 0, 0, 1, 0};
     return b;
 }
 
@@ -759,16 +841,13 @@ cudaError_t launch(const CUtensorMap& map_q, const CUtensorMap& map_k, const CUt
 }
 
 template <int kRequests>
-cudaError_t finish(const ChunkParams& p, const Batch<ChunkReq, kManyRequests>& batch, cudaStream_t stream, bool mass) {
-    long long rows = 0, len = 0;
-    for (int i = 0; i < batch.n; ++i) {
-        if (batch.r[i].splits > 1) rows = std::max(rows, (long long)batch.r[i].n_new * p.pages.n_q_heads);
-        len = std::max<long long>(len, batch.r[i].len);
-    }
-    if (mass)
-        return launch_chained(step_mass_kernel<kRequests>, dim3((unsigned)((len + kMassRows - 1) / kMassRows * p.pages.n_kv_heads), batch.n),
-                              dim3(kFinishThreads), 0, stream, p, shorter<kRequests>(batch));
-    return launch_chained(chunk_finish_kernel<kRequests>, dim3((unsigned)std::min<long long>((rows + kFinishWarps - 1) / kFinishWarps, 4096), batch.n),
+cudaError_t finish(const ChunkParams& p, const Batch<ChunkReq, kManyRequests>& batch, cudaStream_t stream) {
+    int len = 0;
+    for (int i = 0; i < batch.n; ++i) len = std::max(len, batch.r[i].len);
+    if (p.mass)
+        return launch_chained(chunk_finish_kernel<kRequests, true>, dim3(p.n_units, (len + kMassRows - 1) / kMassRows), dim3(kFinishThreads), 0,
+                              stream, p, shorter<kRequests>(batch));
+    return launch_chained(chunk_finish_kernel<kRequests, false>, dim3(p.n_units, (p.slot_rows + kFinishWarps - 1) / kFinishWarps),
                           dim3(kFinishThreads), 0, stream, p, shorter<kRequests>(batch));
 }
 
@@ -784,11 +863,8 @@ cudaError_t launch_chunk(const CUtensorMap& map_q, const CUtensorMap& map_k, con
                : launch<kManyRequests, false>(map_q, map_k, map_v, p, batch, grid, stream);
 }
 
-cudaError_t launch_chunk_ranges(const ChunkParams& p, const Batch<ChunkReq, kManyRequests>& batch, cudaStream_t stream) {
-    return batch.n <= kFewRequests ? finish<kFewRequests>(p, batch, stream, false) : finish<kManyRequests>(p, batch, stream, false);
-}
-cudaError_t launch_step_mass(const ChunkParams& p, const Batch<ChunkReq, kManyRequests>& batch, cudaStream_t stream) {
-    return batch.n <= kFewRequests ? finish<kFewRequests>(p, batch, stream, true) : finish<kManyRequests>(p, batch, stream, true);
+cudaError_t launch_chunk_finish(const ChunkParams& p, const Batch<ChunkReq, kManyRequests>& batch, cudaStream_t stream) {
+    return batch.n <= kFewRequests ? finish<kFewRequests>(p, batch, stream) : finish<kManyRequests>(p, batch, stream);
 }
 
 }  // namespace lookm

@@ -119,8 +119,8 @@ evict_copy_kernel(const EvictParams p, const __grid_constant__ Batch<EvictReq, k
     const int h = blockIdx.y, l = threadIdx.x & 15;
     constexpr int kRows = kMoveThreads / 16 * kMoveRows;
     const int i0 = blockIdx.x * kRows + (threadIdx.x >> 4);
-    if (blockIdx.x * kRows >= rq.budget) return;
     grid_dependency_wait();
+    if (blockIdx.x * kRows >= rq.budget) return;
     const int* kept = p.kept + rq.kept_off + (long long)h * rq.budget;
     Pages out = p.pages;
     out.table = p.out_table;

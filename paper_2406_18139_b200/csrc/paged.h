@@ -73,34 +73,64 @@ struct ChunkReq {
     int q_begin, n_new;          // its tokens on the packed axis
     int len;                     // cached rows, the new ones included
     int index;                   // of the request in the page table
-    int item_begin;              // first work item
+    int unit_begin;              // units of the launch before its own
     int n_sets;                  // two query tiles each, the last perhaps one
-    int splits;                  // ranges that the cached rows are cut into
-    int pad;
-    long long part_begin;        // splits > 1: first partial row, in rows: [split][token][query head]
-    long long logits_begin;      // steps: first logit of its [query head][row] block
+    int step_begin;              // shares: steps of the launch before its own
+    int head_steps;              // shares: steps of one of its KV heads
+    long long logits_begin;      // steps with weights: first logit of its [query head][row] block
 };
+// A unit of work: a set of query tiles of a KV head.
+struct ChunkUnit {
+    int tok0;                    // first token
+    bool pair;                   // two query tiles
+    int tiles0, tiles;           // tiles of cached rows that its first query tile sees, that it sees
+    int steps;                   // its share of the work: so many for itself, and one per tile and query tile
+};
+constexpr int kUnitSteps = 2;
+#ifdef __CUDACC__
+__host__ __device__
+#endif
+inline ChunkUnit chunk_unit(const ChunkReq& q, int set, int tile_tokens) {
+    ChunkUnit u;
+    u.tok0 = set * 2 * tile_tokens;
+    u.pair = u.tok0 + tile_tokens < q.n_new;
+    const int before = q.len - q.n_new, first = u.tok0 + tile_tokens, second = first + tile_tokens;
+    u.tiles0 = (before + (first < q.n_new ? first : q.n_new) + kTile - 1) / kTile;
+    u.tiles = u.pair ? (before + (second < q.n_new ? second : q.n_new) + kTile - 1) / kTile : u.tiles0;
+    u.steps = kUnitSteps + (u.pair ? 2 : 1) * u.tiles;
+    return u;
+}
+// The tile at which a cut after `local` of a unit's steps falls.
+#ifdef __CUDACC__
+__host__ __device__
+#endif
+inline int chunk_cut(const ChunkUnit& u, int local) {
+    if (local >= u.steps) return u.tiles;
+    const int t = (local - kUnitSteps) / (u.pair ? 2 : 1);
+    return t > 0 ? t : 0;
+}
 struct ChunkParams {
     Pages pages;
     int group, tile_tokens;      // query heads of a KV head, tokens of a query tile
-    int n_items;
+    int n_units;
     int n_tokens;                // on the packed axis (= the row stride of lse)
+    int share;                   // > 0: the CTAs take so many steps each of all units' ...
+    int total_steps;             // ... which are so many; units that are cut leave partial rows
+    int slot_rows;               // partial rows of a piece: two pieces per CTA, its first and its last
     float scale_log2;            // softmax scale * log2(e)
     const void* cache_v;
     void* out;                   // [tokens, n_q_heads, 128] bf16
     float* lse;                  // [n_q_heads, tokens] or NULL
-    float* part_out;             // partial rows, normalised: [row][128]
+    float* part_out;             // partial rows, normalised: [piece][row][128]
     float* part_lse;             // their log2-sum-exp2
-    float* logits;               // steps: q.k of every row (unscaled)
-    float* mass;                 // steps
+    float* logits;               // steps with weights: q.k of every row (unscaled)
+    float* mass;                 // steps with weights
     int* status;
 };
 cudaError_t launch_chunk(const CUtensorMap& map_q, const CUtensorMap& map_k, const CUtensorMap& map_v, const ChunkParams& p,
                          const Batch<ChunkReq, kManyRequests>& batch, int grid, cudaStream_t stream);
-// Adds up the ranges of requests that have several.
-cudaError_t launch_chunk_ranges(const ChunkParams& p, const Batch<ChunkReq, kManyRequests>& batch, cudaStream_t stream);
-// Steps: adds every row's weight to its mass.
-cudaError_t launch_step_mass(const ChunkParams& p, const Batch<ChunkReq, kManyRequests>& batch, cudaStream_t stream);
+// Adds up the pieces of units that were cut, and with p.mass every row's weight to its mass.
+cudaError_t launch_chunk_finish(const ChunkParams& p, const Batch<ChunkReq, kManyRequests>& batch, cudaStream_t stream);
 
 // ---- evict_kernels.cu ------------------------------------------------------------------------------
 struct EvictReq {

@@ -210,83 +210,43 @@ int evict(const void* cache_k, const void* cache_v, const float* mass, const int
 }
 
 // ---- attention of the newest tokens -----------------------------------------------------------------
-constexpr int kMaxRanges = 64;           // of the cached rows of an item
-constexpr int kMinRangeTiles = 2;        // tiles of cached rows in a range, at least
-constexpr int kMaxRangeItems = 640;      // items of a call that has ranges
+constexpr int kMaxCtas = 192;            // of a launch
 
-struct ChunkPlan {
-    std::vector<ChunkReq> reqs;          // longest items first
-    int tile_tokens = 1;
-    bool ranges = false;
-    size_t o_parts, o_part_lse, o_logits, o_lse, total;
-};
-
-// Tiles of cached rows that the item of a request's last set streams, and its work: tiles times query tiles.
-struct Longest { int tiles, steps; };
-Longest longest_item(const ChunkReq& q, int tile_tokens) {
-    const int tiles = (q.len + kTile - 1) / kTile, last = (q.n_new + tile_tokens - 1) / tile_tokens;
-    return {tiles, last > 1 ? 2 * tiles : tiles};
-}
-
-size_t part_rows_bound(const lookm_paged_layout* l, int n, const int* new_lens, const int* lens) {
-    size_t rows = 0;
-    for (int r = 0; r < n; ++r) {
-        const size_t ranges = std::min<size_t>(kMaxRanges, ((size_t)lens[r] + kMinRangeTiles * kTile - 1) / (kMinRangeTiles * kTile));
-        rows += (new_lens ? (size_t)std::max(new_lens[r], 1) : 1) * l->n_q_heads * ranges;
-    }
-    return std::min<size_t>(rows, (size_t)kMaxRangeItems * 2 * kTile);
-}
-
-size_t chunk_workspace(size_t part_rows, size_t logits, size_t lse, ChunkPlan* pl) {
+// The workspace behind the status word: partial rows of the pieces (two a CTA), logits and log-sum-exps of a step.
+struct ChunkSpace { size_t parts, part_lse, logits, lse, total; };
+ChunkSpace chunk_space(size_t slot_rows, size_t logits, size_t lse) {
     size_t o = kStatusBytes;
     auto carve = [&](size_t bytes) { size_t at = o; o = align_up(o + bytes, 256); return at; };
-    const size_t parts = carve(4 * part_rows * kHeadDim), part_lse = carve(4 * part_rows), lo = carve(4 * logits), ls = carve(4 * lse);
-    if (pl) {
-        pl->o_parts = parts;
-        pl->o_part_lse = part_lse;
-        pl->o_logits = lo;
-        pl->o_lse = ls;
-        pl->total = o;
-    }
-    return o;
+    ChunkSpace w;
+    w.parts = carve(4 * kHeadDim * 2 * kMaxCtas * slot_rows);
+    w.part_lse = carve(4 * 2 * kMaxCtas * slot_rows);
+    w.logits = carve(4 * logits);
+    w.lse = carve(4 * lse);
+    w.total = o;
+    return w;
+}
+int slot_rows(const lookm_paged_layout* l, long long most_new) {
+    const int group = l->n_q_heads / l->n_kv_heads;
+    return (int)std::min<long long>(2ll * (kTile / group) * group, std::max<long long>(most_new, 1) * group);
 }
 
-// How the rows are cut.  Enough items for the SMs: not at all.  Else into ranges, so that all items together are one wave,
-// or, where the items alone are more than a wave, none is longer than half of what an SM has to do.
-void plan_ranges(ChunkPlan& pl, const lookm_paged_layout* l, int sms) {
-    long long items = 0, steps = 0;
-    for (const ChunkReq& q : pl.reqs) {
-        const Longest it = longest_item(q, pl.tile_tokens);
-        items += (long long)l->n_kv_heads * q.n_sets;
-        steps += (long long)l->n_kv_heads * q.n_sets * it.steps;
-    }
-    if (items == 0 || items >= kMaxRangeItems / 2) return;
-    const auto ranges = [&](const ChunkReq& q, long long limit) {
-        const Longest it = longest_item(q, pl.tile_tokens);
-        const long long most = std::min<long long>(kMaxRanges, (it.tiles + kMinRangeTiles - 1) / kMinRangeTiles);
-        return (int)std::max<long long>(1, std::min<long long>(most, (it.steps + limit - 1) / limit));
-    };
-    const auto count = [&](long long limit) {
-        long long n = 0;
-        for (const ChunkReq& q : pl.reqs) n += (long long)l->n_kv_heads * q.n_sets * ranges(q, limit);
-        return n;
-    };
-    long long limit = std::max<long long>(1, steps / sms);
-    if (items <= sms) {
-        long long lo = limit, hi = 2ll * ((1ll << 30) / kTile + 1);
-        while (lo < hi) {
-            const long long mid = lo + (hi - lo) / 2;
-            if (count(mid) > sms) lo = mid + 1; else hi = mid;
+// Whether the CTAs of a launch take equal shares of all units' steps instead of whole units: where the longest of these
+// would keep its SM busy for longer than a share and a second launch.
+bool takes_shares(const ChunkReq* reqs, int n, int tile_tokens, int heads, int rows, int sms, long long* total) {
+    long long units = 0, steps = 0, longest = 0;
+    for (int r = 0; r < n; ++r) {
+        units += (long long)reqs[r].n_sets * heads;
+        if (units >= 4ll * sms) return false;
+        for (int s = 0; s < reqs[r].n_sets; ++s) {
+            const int k = chunk_unit(reqs[r], s, tile_tokens).steps;
+            steps += (long long)k * heads;
+            longest = std::max<long long>(longest, k);
         }
-        limit = lo;
-    } else {
-        limit = std::max<long long>(1, limit / 2);
-        while (count(limit) > kMaxRangeItems) limit *= 2;
     }
-    for (ChunkReq& q : pl.reqs) {
-        q.splits = ranges(q, limit);
-        pl.ranges = pl.ranges || q.splits > 1;
-    }
+    *total = steps;
+    if (steps >= (1ll << 30)) return false;
+    const long long share = (steps + sms - 1) / sms, whole = units <= sms ? longest : std::max(longest, share + longest / 2);
+    return whole > share + 6 + rows / 16;
 }
 
 // bf16 [tokens, heads, 128]: boxes of the rows of a query tile
@@ -330,82 +290,81 @@ int chunk_attention(const void* q, const void* cache_k, const void* cache_v, flo
     LOOKM_TRY(check_pool(cache_k, cache_v, table));
     const int group = paged->n_q_heads / paged->n_kv_heads;
     const long long tokens = step ? n : cu[n];
-    ChunkPlan pl;
-    pl.tile_tokens = kTile / group;
-    long long logits = 0, part_rows = 0, max_items = 0;
+    const int tile_tokens = kTile / group;
+    std::vector<ChunkReq> reqs;
+    long long logits = 0, most_new = 0, units = 0;
     for (int r = 0; r < n; ++r) {
         ChunkReq c;
         c.q_begin = step ? r : cu[r];
         c.n_new = step ? 1 : cu[r + 1] - cu[r];
         c.len = lens[r];
         c.index = r;
-        c.item_begin = 0;
-        c.n_sets = ((c.n_new + pl.tile_tokens - 1) / pl.tile_tokens + 1) / 2;
-        c.splits = 1;
-        c.pad = 0;
-        c.part_begin = 0;
+        c.n_sets = ((c.n_new + tile_tokens - 1) / tile_tokens + 1) / 2;
+        c.unit_begin = c.step_begin = c.head_steps = 0;
         c.logits_begin = logits;
         if (c.len < c.n_new) return LOOKM_ERR_INVALID_ARG;
         logits += step ? (long long)c.len * paged->n_q_heads : 0;
-        if (c.n_new) pl.reqs.push_back(c);
-        max_items += (long long)c.n_sets * paged->n_kv_heads;
+        if (c.n_new) reqs.push_back(c);
+        most_new = std::max<long long>(most_new, c.n_new);
+        units += (long long)c.n_sets * paged->n_kv_heads;
     }
-    if (max_items + kMaxRangeItems >= (1ll << 31) || tokens * paged->n_q_heads >= (1ll << 40)) return LOOKM_ERR_UNSUPPORTED;
+    if (units + kMaxCtas >= (1ll << 31) || tokens * paged->n_q_heads >= (1ll << 40)) return LOOKM_ERR_UNSUPPORTED;
+    const int rows = slot_rows(paged, most_new);
+    const ChunkSpace space = chunk_space(rows, logits, step && !lse ? tokens * paged->n_q_heads : 0);
+    LOOKM_TRY(check_ws(ws, ws_bytes, space.total));
     DeviceInfo di;
-    const int known = device_info(di);           // (asked again below: the plan needs no device)
-    plan_ranges(pl, paged, known == LOOKM_OK && di.sms > 0 ? di.sms : 148);
-    for (ChunkReq& c : pl.reqs) {
-        c.part_begin = part_rows;
-        if (c.splits > 1) part_rows += (long long)c.splits * c.n_new * paged->n_q_heads;
-    }
-    chunk_workspace(part_rows, logits, step && !lse ? tokens * paged->n_q_heads : 0, &pl);
-    LOOKM_TRY(check_ws(ws, ws_bytes, pl.total));
-    LOOKM_TRY(known);
+    LOOKM_TRY(device_info(di));
     g_launches = 0;
-    if (pl.reqs.empty()) return LOOKM_OK;
-    std::stable_sort(pl.reqs.begin(), pl.reqs.end(), [&](const ChunkReq& a, const ChunkReq& b) {
-        return (long long)longest_item(a, pl.tile_tokens).steps * b.splits > (long long)longest_item(b, pl.tile_tokens).steps * a.splits;
-    });
+    if (reqs.empty()) return LOOKM_OK;
+    std::stable_sort(reqs.begin(), reqs.end(), [](const ChunkReq& a, const ChunkReq& b) { return a.len > b.len; });
     CUtensorMap map_q, map_k, map_v;
-    LOOKM_TRY(make_map_q(&map_q, q, tokens, paged, group, pl.tile_tokens));
+    LOOKM_TRY(make_map_q(&map_q, q, tokens, paged, group, tile_tokens));
     LOOKM_TRY(make_map_pool(&map_k, cache_k, paged));
     LOOKM_TRY(make_map_pool(&map_v, cache_v, paged));
     ChunkParams p;
     p.pages = pages_of(paged, table);
     p.group = group;
-    p.tile_tokens = pl.tile_tokens;
+    p.tile_tokens = tile_tokens;
+    p.slot_rows = rows;
     p.n_tokens = (int)tokens;
     p.scale_log2 = (paged->softmax_scale > 0.f ? paged->softmax_scale : 1.0f / std::sqrt((float)kHeadDim)) * 1.4426950408889634f;
     p.cache_v = cache_v;
     p.out = out;
-    p.lse = lse ? lse : step ? at<float>(ws, pl.o_lse) : nullptr;
-    p.part_out = at<float>(ws, pl.o_parts);
-    p.part_lse = at<float>(ws, pl.o_part_lse);
-    p.logits = step ? at<float>(ws, pl.o_logits) : nullptr;
+    p.lse = lse ? lse : step ? at<float>(ws, space.lse) : nullptr;
+    p.part_out = at<float>(ws, space.parts);
+    p.part_lse = at<float>(ws, space.part_lse);
+    p.logits = step ? at<float>(ws, space.logits) : nullptr;
     p.mass = mass;
     p.status = at<int>(ws, 0);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    for (size_t base = 0; base < pl.reqs.size(); base += kManyRequests) {
+    const int sms = std::min(di.sms, kMaxCtas), heads = paged->n_kv_heads;
+    for (size_t base = 0; base < reqs.size(); base += kManyRequests) {
         Batch<ChunkReq, kManyRequests> b;
-        b.n = (int)std::min<size_t>(kManyRequests, pl.reqs.size() - base);
+        b.n = (int)std::min<size_t>(kManyRequests, reqs.size() - base);
         b.pad = 0;
-        long long items = 0;
-        bool ranges = false;
+        long long total = 0;
+        const bool shares = takes_shares(&reqs[base], b.n, tile_tokens, heads, rows, sms, &total);
+        int ctas = sms;
+        p.n_units = p.share = p.total_steps = 0;
+        if (shares) {
+            p.total_steps = (int)total;
+            p.share = (int)((total + sms - 1) / sms);
+            ctas = (int)((total + p.share - 1) / p.share);
+        }
+        int at_step = 0;
         for (int i = 0; i < b.n; ++i) {
-            b.r[i] = pl.reqs[base + i];
-            b.r[i].item_begin = (int)items;
-            items += (long long)b.r[i].n_sets * b.r[i].splits * paged->n_kv_heads;
-            ranges = ranges || b.r[i].splits > 1;
+            ChunkReq& c = b.r[i] = reqs[base + i];
+            c.unit_begin = p.n_units;
+            p.n_units += c.n_sets * heads;
+            if (!shares) continue;
+            for (int s = 0; s < c.n_sets; ++s) c.head_steps += chunk_unit(c, s, tile_tokens).steps;
+            c.step_begin = at_step;
+            at_step += c.head_steps * heads;
         }
-        p.n_items = (int)items;
-        LOOKM_CUDA(launch_chunk(map_q, map_k, map_v, p, b, (int)std::min<long long>(items, di.sms), st));
+        LOOKM_CUDA(launch_chunk(map_q, map_k, map_v, p, b, std::min(ctas, shares ? ctas : p.n_units), st));
         ++g_launches;
-        if (ranges) {
-            LOOKM_CUDA(launch_chunk_ranges(p, b, st));
-            ++g_launches;
-        }
-        if (step) {
-            LOOKM_CUDA(launch_step_mass(p, b, st));
+        if (shares || step) {
+            LOOKM_CUDA(launch_chunk_finish(p, b, st));
             ++g_launches;
         }
     }
@@ -428,8 +387,10 @@ size_t lookm_paged_workspace_size(const lookm_paged_layout* paged, int n_request
         rows += cache_lens_host[r];
         tokens += new_lens_host ? new_lens_host[r] : 1;
     }
-    const size_t attention = chunk_workspace(part_rows_bound(paged, n_requests, new_lens_host, cache_lens_host), rows * paged->n_q_heads,
-                                             std::max(tokens, (size_t)n_requests) * paged->n_q_heads, nullptr);
+    long long most_new = 1;
+    for (int r = 0; r < n_requests; ++r) most_new = std::max<long long>(most_new, new_lens_host ? new_lens_host[r] : 1);
+    const size_t attention = chunk_space(slot_rows(paged, most_new), rows * paged->n_q_heads,
+                                         std::max(tokens, (size_t)n_requests) * paged->n_q_heads).total;
     return std::max(align_up(kStatusBytes + 4 * rows * paged->n_kv_heads, 256), attention);
 }
 
