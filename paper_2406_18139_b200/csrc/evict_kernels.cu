@@ -13,6 +13,7 @@ namespace lookm {
 namespace {
 
 constexpr int kSelThreads = 1024, kSelWarps = kSelThreads / 32;
+constexpr int kHistCopies = 4;                   // warps that would count in the same word wait for one another
 
 // Masses in an order that unsigned integers have: -0 as +0, NaN below everything.  Never 0: that is for rows beyond the candidates.
 __device__ __forceinline__ uint32_t key_of(float x) {
@@ -21,22 +22,12 @@ __device__ __forceinline__ uint32_t key_of(float x) {
     return (b & 0x80000000u) ? max(~b, 2u) : b | 0x80000000u;
 }
 
-// Sums of up to three counters over the CTA; two buffers, so that one barrier a call is enough.
-__device__ __forceinline__ void block_sum3(int (&c)[3], int (*buf)[3]) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-#pragma unroll
-    for (int i = 0; i < 3; ++i) c[i] = __reduce_add_sync(0xffffffffu, c[i]);
-    if (lane < 3) buf[warp][lane] = lane == 0 ? c[0] : lane == 1 ? c[1] : c[2];
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 3; ++i) c[i] = __reduce_add_sync(0xffffffffu, buf[lane][i]);
-}
-
 // kKeys > 0: so many candidates per thread, whose keys stay in registers; 0: any number, read again in every pass.
 template <int kKeys, int kRequests>
 __global__ void __launch_bounds__(kSelThreads)
 evict_select_kernel(const EvictParams p, const __grid_constant__ Batch<EvictReq, kRequests> batch) {
-    __shared__ int buf[2][kSelWarps][3];
+    __shared__ int hist[kHistCopies][256];
+    __shared__ int warp_total[8], found[2];
     __shared__ int2 warp_count[kSelWarps];
     const EvictReq& rq = batch.r[blockIdx.y];
     const int h = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -70,17 +61,41 @@ evict_select_kernel(const EvictParams p, const __grid_constant__ Batch<EvictReq,
             for (int s = 0; s < steps; ++s) f(s, read(s));
         }
     };
-    // The n_top-th largest key, two bits a step: the largest x with at least n_top keys >= x.
+    // The n_top-th largest key, eight bits a step: counts of the digit among the keys that begin with what is known of it.  (Two
+    // bits a step by counting in registers took four times as long: three reductions per warp and step.)
     uint32_t x = 0;
-    int turn = 0;
-    for (int bit = 30; bit >= 0; bit -= 2, turn ^= 1) {
-        const uint32_t a = x | (1u << bit), b = x | (2u << bit), c = x | (3u << bit);
-        int n[3] = {0, 0, 0};
-        for_each([&](int, uint32_t k) { n[0] += k >= a; n[1] += k >= b; n[2] += k >= c; });
-        block_sum3(n, buf[turn]);
-        if (n[2] >= n_top) x = c;
-        else if (n[1] >= n_top) x = b;
-        else if (n[0] >= n_top) x = a;
+    int want = n_top;                            // its rank among these keys
+    for (int shift = 24; shift >= 0; shift -= 8) {
+        for (int i = threadIdx.x; i < kHistCopies * 256; i += kSelThreads) (&hist[0][0])[i] = 0;
+        __syncthreads();
+        for_each([&](int, uint32_t k) {
+            if (k != 0 && (shift == 24 || (k ^ x) >> (shift + 8) == 0)) atomicAdd(&hist[warp % kHistCopies][(k >> shift) & 255], 1);
+        });
+        __syncthreads();
+        int n = 0, at_least = 0;                 // keys with this thread's digit, keys of the warp's with it or a larger one
+        const int digit = 255 - threadIdx.x;
+        if (threadIdx.x < 256) {
+#pragma unroll
+            for (int i = 0; i < kHistCopies; ++i) n += hist[i][digit];
+            at_least = n;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int y = __shfl_up_sync(0xffffffffu, at_least, d);
+                if (lane >= d) at_least += y;
+            }
+            if (lane == 31) warp_total[warp] = at_least;
+        }
+        __syncthreads();
+        if (threadIdx.x < 256) {
+            for (int i = 0; i < warp; ++i) at_least += warp_total[i];
+            if (at_least >= want && at_least - n < want) {
+                found[0] = digit;
+                found[1] = want - (at_least - n);
+            }
+        }
+        __syncthreads();
+        x |= (uint32_t)found[0] << shift;
+        want = found[1];
     }
     // Rows above it all stay; of those equal to it the lowest that there is room for.
     int2 mine = {0, 0};                          // above, equal: of the warp
@@ -159,46 +174,56 @@ evict_copy_kernel(const EvictParams p, const __grid_constant__ Batch<EvictReq, k
 // In place.  A CTA takes a slice of 1 / kSlices of the features of all kept rows of one pool's head, in ascending order and a
 // batch at a time: all loads of a batch, a barrier, its stores.  Row i comes from row kept[i] >= i, so a store never
 // hits a row that a later batch still reads, and other CTAs touch other bytes.
-constexpr int kPlaceRows = 8;                    // of a thread at a time
+// The next batch's rows are asked for before this one's are stored.
+constexpr int kPlaceRows = 4;                    // of a thread at a time
 template <int kSlices, int kRequests>
 __global__ void __launch_bounds__(kMoveThreads)
 evict_in_place_kernel(const EvictParams p, const __grid_constant__ Batch<EvictReq, kRequests> batch) {
-    constexpr int kLanes = 16 / kSlices, kGroups = kMoveThreads / kLanes;        // lanes of a row, rows side by side
+    constexpr int kLanes = 16 / kSlices, kGroups = kMoveThreads / kLanes, kStep = kGroups * kPlaceRows;   // lanes of a row, rows side by side
     const EvictReq& rq = batch.r[blockIdx.z];
     const int h = blockIdx.y, slice = blockIdx.x >> 1;
-    const bool is_v = blockIdx.x & 1, has_mass = blockIdx.x == 0;
+    const bool is_v = blockIdx.x & 1, has_mass = blockIdx.x == 0 && threadIdx.x % kLanes == 0;
     grid_dependency_wait();
     const int* kept = p.kept + rq.kept_off + (long long)h * rq.budget;
     Pages out = p.pages;
     out.table = p.out_table;
-    const char* in = static_cast<const char*>(is_v ? p.cache_v : p.cache_k);
-    char* to_pool = static_cast<char*>(is_v ? p.out_v : p.out_k);
-    const int l = (slice * kLanes + threadIdx.x % kLanes) * 16;
-    for (int base = 0; base < rq.budget; base += kGroups * kPlaceRows) {
+    const char* in = static_cast<const char*>(is_v ? p.cache_v : p.cache_k) + (slice * kLanes + threadIdx.x % kLanes) * 16;
+    char* to_pool = static_cast<char*>(is_v ? p.out_v : p.out_k) + (slice * kLanes + threadIdx.x % kLanes) * 16;
+    struct Rows {
         uint4 x[kPlaceRows];
         float m[kPlaceRows];
-        long long to[kPlaceRows], to_mass[kPlaceRows];
+        int page[kPlaceRows];                    // where they go; -1: nowhere
+    } now, next;
+    const auto ask = [&](int base, Rows& b) {
+        int from[kPlaceRows];
 #pragma unroll
         for (int j = 0; j < kPlaceRows; ++j) {
-            const int i = base + j * kGroups + threadIdx.x / kLanes, from = i < rq.budget ? kept[i] : -1;
-            to[j] = -1;
-            if (from < 0) continue;
-            const int src = p.pages.page_of(rq.index, from, p.status), dst = out.page_of(rq.index, i, p.status);
-            if (src < 0 || dst < 0) continue;
-            x[j] = *reinterpret_cast<const uint4*>(in + 2 * p.pages.row_at(src, from, h) + l);
-            to[j] = 2 * out.row_at(dst, i, h) + l;
-            if (has_mass) {
-                m[j] = p.mass[p.pages.mass_at(src, from, h)];
-                to_mass[j] = out.mass_at(dst, i, h);
-            }
+            const int i = base + j * kGroups + threadIdx.x / kLanes;
+            from[j] = i < rq.budget ? kept[i] : -1;
         }
+#pragma unroll
+        for (int j = 0; j < kPlaceRows; ++j) {
+            b.page[j] = -1;
+            if (from[j] < 0) continue;
+            const int src = p.pages.page_of(rq.index, from[j], p.status);
+            if (src < 0) continue;
+            b.page[j] = out.page_of(rq.index, base + j * kGroups + threadIdx.x / kLanes, p.status);
+            b.x[j] = *reinterpret_cast<const uint4*>(in + 2 * p.pages.row_at(src, from[j], h));
+            if (has_mass) b.m[j] = p.mass[p.pages.mass_at(src, from[j], h)];
+        }
+    };
+    ask(0, now);
+    for (int base = 0; base < rq.budget; base += kStep) {
+        if (base + kStep < rq.budget) ask(base + kStep, next);
         __syncthreads();
 #pragma unroll
         for (int j = 0; j < kPlaceRows; ++j) {
-            if (to[j] < 0) continue;
-            *reinterpret_cast<uint4*>(to_pool + to[j]) = x[j];
-            if (has_mass && threadIdx.x % kLanes == 0) p.out_mass[to_mass[j]] = m[j];
+            const int i = base + j * kGroups + threadIdx.x / kLanes;
+            if (now.page[j] < 0) continue;
+            *reinterpret_cast<uint4*>(to_pool + 2 * out.row_at(now.page[j], i, h)) = now.x[j];
+            if (has_mass) p.out_mass[out.mass_at(now.page[j], i, h)] = now.m[j];
         }
+        now = next;
     }
 }
 
