@@ -142,6 +142,8 @@ def _c_array(ctype, code, seq):
     take as integers is converted one by one."""
     if not isinstance(seq, (list, tuple)):
         seq = list(seq)                  # an iterator can be walked once only; bytes are their values here
+    if len(seq) <= 3:                    # 0.4 us; 0.65 through an array
+        return (ctype * len(seq))(*[int(x) for x in seq])
     try:
         values = array(code, seq)
         return (ctype * len(values)).from_buffer(values)
@@ -400,20 +402,22 @@ def make_append_options(q_weight=None, k_weight=None, eps: float = 0.0, inv_freq
     return AppendOptions(_ptr(q_weight), _ptr(k_weight), float(eps), 0 if freq is None else 2 * len(freq), int(bool(interleaved)), freq)
 
 
-def _here(tensors, n: int, page_table, *lists) -> bool:
-    """Whether all tensors are on the current device, where the call would run, and the host lists and the table's rows
-    are as many as the n requests (the library reads them by pointer and can't tell)."""
+def _here(n: int, page_table, tensors) -> bool:
+    """Whether all tensors are on the current device, where the call would run, and the table has a row for each of the n requests
+    (the library reads it by pointer and can't tell)."""
     import torch
     dev = torch._C._cuda_getDevice()
-    return (all(t is None or (t.is_cuda and t.get_device() == dev) for t in tensors) and all(len(x) == n for x in lists)
-            and page_table.dtype == torch.int32 and page_table.shape[0] >= n)
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            return False
+    return page_table.dtype is torch.int32 and page_table.shape[0] >= n
 
 
 def lookm_append_rows(q, k, v, positions, cu_seqlens, cache_lens, layout: Layout, options, q_out, cache_k, cache_v, mass, page_table,
                       paged: PagedLayout, workspace, stream=None):
     """options: an AppendOptions (see make_append_options) or None."""
     n = len(cache_lens)
-    if not _here((q, k, v, positions, q_out, cache_k, cache_v, mass, page_table, workspace), n, page_table, cu_seqlens[1:]):
+    if len(cu_seqlens) != n + 1 or not _here(n, page_table, (q, k, v, positions, q_out, cache_k, cache_v, mass, page_table, workspace)):
         return ERR_INVALID_ARG
     return lib().lookm_append_rows(_ptr(q), _ptr(k), _ptr(v), _ptr(positions), _ints(cu_seqlens), _ints(cache_lens), n,
                                    C.byref(layout), None if options is None else C.byref(options), _ptr(q_out), _ptr(cache_k),
@@ -423,7 +427,7 @@ def lookm_append_rows(q, k, v, positions, cu_seqlens, cache_lens, layout: Layout
 
 def lookm_chunk_attention(q, cache_k, cache_v, page_table, cu_seqlens, cache_lens, paged: PagedLayout, out, lse, workspace, stream=None):
     n = len(cache_lens)
-    if not _here((q, cache_k, cache_v, page_table, out, lse, workspace), n, page_table, cu_seqlens[1:]):
+    if len(cu_seqlens) != n + 1 or not _here(n, page_table, (q, cache_k, cache_v, page_table, out, lse, workspace)):
         return ERR_INVALID_ARG
     return lib().lookm_chunk_attention(_ptr(q), _ptr(cache_k), _ptr(cache_v), _ptr(page_table), _ints(cu_seqlens), _ints(cache_lens), n,
                                        C.byref(paged), _ptr(out), _ptr(lse), _ptr(workspace), _nbytes(workspace), _stream(stream))
@@ -431,7 +435,7 @@ def lookm_chunk_attention(q, cache_k, cache_v, page_table, cu_seqlens, cache_len
 
 def lookm_step_attention(q, cache_k, cache_v, mass, page_table, cache_lens, paged: PagedLayout, out, lse, workspace, stream=None):
     n = len(cache_lens)
-    if not _here((q, cache_k, cache_v, mass, page_table, out, lse, workspace), n, page_table):
+    if not _here(n, page_table, (q, cache_k, cache_v, mass, page_table, out, lse, workspace)):
         return ERR_INVALID_ARG
     return lib().lookm_step_attention(_ptr(q), _ptr(cache_k), _ptr(cache_v), _ptr(mass), _ptr(page_table), _ints(cache_lens), n,
                                       C.byref(paged), _ptr(out), _ptr(lse), _ptr(workspace), _nbytes(workspace), _stream(stream))
@@ -440,8 +444,9 @@ def lookm_step_attention(q, cache_k, cache_v, mass, page_table, cache_lens, page
 def lookm_evict(cache_k, cache_v, mass, page_table, cache_lens, budgets, windows, paged: PagedLayout, out_k, out_v, out_mass,
                 out_page_table, kept_idx, workspace, stream=None):
     n = len(cache_lens)
-    if not _here((cache_k, cache_v, mass, page_table, out_k, out_v, out_mass, out_page_table, kept_idx, workspace), n, page_table,
-                 budgets, windows) or out_page_table.dtype != page_table.dtype or out_page_table.shape[0] < n:
+    if len(budgets) != n or len(windows) != n or not _here(n, page_table, (cache_k, cache_v, mass, page_table, out_k, out_v, out_mass,
+                                                                           out_page_table, kept_idx, workspace)) \
+            or out_page_table.dtype is not page_table.dtype or out_page_table.shape[0] < n:
         return ERR_INVALID_ARG
     return lib().lookm_evict(_ptr(cache_k), _ptr(cache_v), _ptr(mass), _ptr(page_table), _ints(cache_lens), _ints(budgets),
                              _ints(windows), n, C.byref(paged), _ptr(out_k), _ptr(out_v), _ptr(out_mass),

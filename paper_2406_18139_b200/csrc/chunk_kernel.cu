@@ -43,9 +43,10 @@ struct __align__(1024) ChunkShared {
     unsigned long long q_full[2], q_empty[2];
     unsigned long long full[kRing], empty[kRing];
     unsigned long long dirty[kRing];             // V tiles that warps 10 and 11 have to look at; they make them full
-    unsigned long long s_full[2], p_half[2], p_full[2], pv_done[2], o_free[2];
-    unsigned long long merge_full, merge_free, mma_done;
+    unsigned long long s_full[2], p_part[2][2], pv_done[2], o_free[2];         // (p_part: halves of a tile's rows)
+    unsigned long long merge_full, merge_free, lse_full, mma_done;
     float merge_m[kTile], merge_l[kTile];        // one query tile: stream 1's reference and sum
+    float lse2[kTile];                           // steps: the rows' log2-sum-exp2
     int odd_values[kFlags];                      // V had infinities or NaN that were taken out
     uint32_t tmem_base;
     int abort_flag;
@@ -200,14 +201,16 @@ __device__ __forceinline__ void load_tiles(const CUtensorMap& map_q, const CUten
                 ptx::tma_load_3d(dst + kHalfBytes, &map_q, 64, it.head * p.group, tok, bar);
             }
         }
-        const auto load = [&](const CUtensorMap& map, int t, bool dirty) {
+        // The page that this lane fetches for tile t (asked for a tile ahead); beyond the pool, which reads as zeros, if there is none.
+        const auto page_for = [&](int t) {
+            const int row = (it.t0 + t) * kTile + lane * box_rows;
+            if (t >= it.nt || lane >= boxes || row >= it.len) return p.pages.n_pages;
+            const int page = p.pages.page_of(it.index, row, p.status);
+            return page < 0 ? p.pages.n_pages : page;
+        };
+        const auto load = [&](const CUtensorMap& map, int t, int page, bool dirty) {
             if (stop) return;
-            const int s = n % kRing, row = (it.t0 + t) * kTile + lane * box_rows;
-            int page = p.pages.n_pages;          // beyond the pool: reads as zeros
-            if (lane < boxes && row < it.len) {
-                page = p.pages.page_of(it.index, row, p.status);
-                if (page < 0) page = p.pages.n_pages;
-            }
+            const int s = n % kRing;
             if (!warp_wait(&sh.empty[s], ((n / kRing) & 1) ^ 1, abort_flag)) { stop = true; return; }
             const uint32_t bar = ptx::smem_u32(dirty ? &sh.dirty[s] : &sh.full[s]);
             if (lane == 0) {
@@ -219,25 +222,23 @@ __device__ __forceinline__ void load_tiles(const CUtensorMap& map_q, const CUten
             __syncwarp();
             if (lane < boxes) {
                 const uint32_t dst = ptx::smem_u32(&sh.ring[s][0]) + lane * box_rows * 128;
-                const int in_page = row & ((1 << p.pages.page_shift) - 1);
+                const int in_page = ((it.t0 + t) * kTile + lane * box_rows) & ((1 << p.pages.page_shift) - 1);
                 ptx::tma_load_4d(dst, &map, 0, in_page, it.head, page, bar);
                 ptx::tma_load_4d(dst + kHalfBytes, &map, 64, in_page, it.head, page, bar);
             }
             ++n;
         };
-        if (it.pair) {
-            load(map_k, 0, false);
-            for (int t = 0; t < it.nt && !stop; ++t) {
-                load(map_v, t, is_masked(it, t));
-                if (t + 1 < it.nt) load(map_k, t + 1, false);
-            }
-        } else {
-            load(map_k, 0, false);
-            if (it.nt > 1) load(map_k, 1, false);
-            for (int t = 0; t < it.nt && !stop; ++t) {
-                load(map_v, t, is_masked(it, t));
-                if (t + 2 < it.nt) load(map_k, t + 2, false);
-            }
+        // K runs ahead of V by one tile, with one query tile by two
+        int page = page_for(0), page1 = page_for(1), page2 = 0;
+        load(map_k, 0, page, false);
+        if (!it.pair && it.nt > 1) load(map_k, 1, page1, false);
+        for (int t = 0; t < it.nt && !stop; ++t) {
+            page2 = page_for(t + 2);
+            load(map_v, t, page, is_masked(it, t));
+            if (it.pair && t + 1 < it.nt) load(map_k, t + 1, page1, false);
+            if (!it.pair && t + 2 < it.nt) load(map_k, t + 2, page2, false);
+            page = page1;
+            page1 = page2;
         }
     }
     // After an abort: no copy may write shared memory once the CTA has left (bounded, the flag is ignored).
@@ -291,7 +292,7 @@ __device__ __forceinline__ void issue_mmas(const ChunkParams& p, const Batch<Chu
         };
         uint32_t begun = 0;                      // a bit per stream: its output block has something of this item
         const auto pv = [&](int g, uint32_t stage) {             // O of stream g += P x V
-            wait(&sh.p_half[g], (p_phase >> g) & 1);
+            wait(&sh.p_part[g][0], (p_phase >> g) & 1);
             if (stop) return;
             ptx::tc_fence_after_sync();
             const uint64_t b = ptx::umma_desc_sw128_mn(ptx::smem_u32(&sh.ring[stage][0]), kHalfBytes);
@@ -300,7 +301,7 @@ __device__ __forceinline__ void issue_mmas(const ChunkParams& p, const Batch<Chu
 #pragma unroll
                 for (int kk = 0; kk < 4; ++kk) ptx::umma_bf16_ts(d, pr + kk * 8, b + kk * (2048 >> 4), idesc_o, kk > 0 ? 1u : more);
             }
-            wait(&sh.p_full[g], (p_phase >> g) & 1);
+            wait(&sh.p_part[g][1], (p_phase >> g) & 1);
             if (stop) return;
             ptx::tc_fence_after_sync();
             if (leader) {
@@ -426,6 +427,29 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     return *reinterpret_cast<const uint32_t*>(&ab);
 }
 
+// Steps: adds the weights of cached rows t, t + stride, ... < end to their mass, summed over the heads of the group; four rows at a time.
+__device__ __forceinline__ void add_weights(const ChunkParams& p, int index, int head, int len, const float* logits, const float* lse2, int t,
+                                            int end, int stride) {
+    for (; t < end; t += 4 * stride) {
+        int page[4];
+        float w[4] = {0.f, 0.f, 0.f, 0.f}, m[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) page[j] = t + j * stride < end ? p.pages.page_of(index, t + j * stride, p.status) : -1;
+        for (int g = 0; g < p.group; ++g) {
+            float x[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[j] = page[j] >= 0 ? logits[(long long)g * len + t + j * stride] : 0.f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] += ptx::ex2(fmaf(x[j], p.scale_log2, -lse2[g]));
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) m[j] = page[j] >= 0 ? p.mass[p.pages.mass_at(page[j], t + j * stride, head)] : 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (page[j] >= 0) p.mass[p.pages.mass_at(page[j], t + j * stride, head)] = m[j] + w[j];
+    }
+}
+
 // 32 logits of a row as probabilities 2^(s * c + neg), in bf16 pairs; adds them up (before the rounding).
 __device__ __forceinline__ void probabilities(const uint32_t (&s)[32], ptx::f32x2 c, ptx::f32x2 neg, ptx::f32x2 (&sum)[4], uint32_t (&pr)[16]) {
 #pragma unroll
@@ -445,7 +469,7 @@ __device__ __forceinline__ void softmax_rows(const ChunkParams& p, const Batch<C
     const uint32_t ts = tmem + g * kTile + lanes, to = tmem + 2 * kTile + g * kHeadDim + lanes;
     const float c = p.scale_log2;
     const int tok_in_tile = row / p.group, head_in_group = row - tok_in_tile * p.group;
-    uint32_t n = 0, n_items = 0, n_merges = 0;
+    uint32_t n = 0, n_items = 0, n_merges = 0, n_masses = 0;
     Walk walk;
     Item it;
     walk.start(p, batch);
@@ -523,15 +547,15 @@ __device__ __forceinline__ void softmax_rows(const ChunkParams& p, const Batch<C
                     }
                     ptx::tmem_st_wait();
                     ptx::tc_fence_before_sync();
-                    if (h == 0 && lane == 0) ptx::mbar_arrive(ptx::smem_u32(&sh.p_half[g]));
                     __syncwarp();
+                    if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&sh.p_part[g][h]));
                 }
                 const float2 v = ptx::unpack2(ptx::add2(ptx::add2(sum[0], sum[1]), ptx::add2(sum[2], sum[3])));
                 l += v.x + v.y;
             } else if (lane == 0) {
-                ptx::mbar_arrive(ptx::smem_u32(&sh.p_half[g]));
+                ptx::mbar_arrive(ptx::smem_u32(&sh.p_part[g][0]));
+                ptx::mbar_arrive(ptx::smem_u32(&sh.p_part[g][1]));
             }
-            if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&sh.p_full[g]));
             __syncwarp();
         }
         // ---- the item's outputs ----
@@ -630,6 +654,18 @@ __device__ __forceinline__ void softmax_rows(const ChunkParams& p, const Batch<C
             if (two) ptx::mbar_arrive(ptx::smem_u32(&sh.o_free[1]));
         }
         __syncwarp();
+        if constexpr (kStep) {
+            // The weights of a whole unit, by the warps of stream 0; the logits of both streams have been written (stream 1's before merge_full).
+            if (p.mass_inside && !it.partial) {
+                sh.lse2[row] = lse2;
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&sh.lse_full));
+                if (!warp_wait(&sh.lse_full, n_masses & 1, abort_flag)) return;
+                ++n_masses;
+                add_weights(p, it.index, it.head, it.len, p.logits + it.logits_begin + (long long)it.head * p.group * it.len, sh.lse2, row, it.len,
+                            kTile);
+            }
+        }
         ++n_items;
     }
 }
@@ -651,8 +687,8 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
             init(&sh.q_full[i], 1);
             init(&sh.q_empty[i], 1);
             init(&sh.s_full[i], 1);
-            init(&sh.p_half[i], 4);
-            init(&sh.p_full[i], 4);
+            init(&sh.p_part[i][0], 4);
+            init(&sh.p_part[i][1], 4);
             init(&sh.pv_done[i], 1);
             init(&sh.o_free[i], 4);
         }
@@ -663,6 +699,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
         }
         init(&sh.merge_full, 4);
         init(&sh.merge_free, 4);
+        init(&sh.lse_full, 4);
         init(&sh.mma_done, 1);
         for (int i = 0; i < kFlags; ++i) sh.odd_values[i] = 0;
         sh.abort_flag = 0;
@@ -701,7 +738,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
 
 // ---- pieces added up, weights accumulated -----------------------------------------------------------
 constexpr int kFinishThreads = 256, kFinishWarps = kFinishThreads / 32;
-constexpr int kMassRows = 2 * kFinishThreads;    // cached rows of a CTA
+constexpr int kMassRows = 4 * kFinishThreads;    // cached rows of a CTA
 
 // What a unit was cut into: CTAs first .. last, some of which may have none of its tiles.
 struct Cuts {
@@ -781,7 +818,7 @@ __device__ __forceinline__ void add_pieces(const ChunkParams& p, const ChunkReq&
 
 // blockIdx.x: unit; blockIdx.y: its rows in turn, or with weights blocks of cached rows (of which the first also has the rows).
 template <int kRequests, bool kStep>
-__global__ void __launch_bounds__(kFinishThreads)
+__global__ void __launch_bounds__(kFinishThreads, 4)
 chunk_finish_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__ Batch<ChunkReq, kRequests> batch) {
     __shared__ float lse2[kTile];
     int lo = 0, hi = batch.n - 1;
@@ -793,7 +830,7 @@ chunk_finish_kernel(const __grid_constant__ ChunkParams p, const __grid_constant
     const int k = blockIdx.x - q.unit_begin, head = k % p.pages.n_kv_heads, warp = threadIdx.x >> 5;
     const Cuts cuts(p, q, head, k / p.pages.n_kv_heads);
     grid_dependency_wait();                      // (also by CTAs that leave: this grid's end has to mean the end of the one before it)
-    if (kStep ? (long long)blockIdx.y * kMassRows >= q.len : cuts.pieces == 1) return;
+    if (kStep ? (long long)blockIdx.y * kMassRows >= q.len || (p.mass_inside && cuts.pieces == 1) : cuts.pieces == 1) return;
     if (cuts.pieces > 1) {
         const int rows = min(q.n_new - cuts.u.tok0, 2 * p.tile_tokens) * p.group;
         if (!kStep || blockIdx.y == 0)
@@ -808,13 +845,9 @@ chunk_finish_kernel(const __grid_constant__ ChunkParams p, const __grid_constant
             if ((threadIdx.x & 31) == 0) lse2[g] = x;
         }
         __syncthreads();
-        for (int t = blockIdx.y * kMassRows + threadIdx.x; t < min(q.len, ((int)blockIdx.y + 1) * kMassRows); t += kFinishThreads) {
-            const int page = p.pages.page_of(q.index, t, p.status);
-            const float* logits = p.logits + q.logits_begin + (long long)head * p.group * q.len + t;
-            float w = 0.f;
-            for (int g = 0; g < p.group; ++g) w += ptx::ex2(fmaf(logits[(long long)g * q.len], p.scale_log2, -lse2[g]));
-            if (page >= 0) p.mass[p.pages.mass_at(page, t, head)] += w;
-        }
+        const int t0 = blockIdx.y * kMassRows;
+        add_weights(p, q.index, head, q.len, p.logits + q.logits_begin + (long long)head * p.group * q.len, lse2, t0 + threadIdx.x,
+                    min(q.len, t0 + kMassRows), kFinishThreads);
     }
 }
 

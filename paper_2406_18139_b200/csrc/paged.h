@@ -106,7 +106,7 @@ __host__ __device__
 #endif
 inline int chunk_cut(const ChunkUnit& u, int local) {
     if (local >= u.steps) return u.tiles;
-    const int t = (local - kUnitSteps) / (u.pair ? 2 : 1);
+    const int t = (local - kUnitSteps) >> (u.pair ? 1 : 0);
     return t > 0 ? t : 0;
 }
 struct ChunkParams {
@@ -125,6 +125,7 @@ struct ChunkParams {
     float* part_lse;             // their log2-sum-exp2
     float* logits;               // steps with weights: q.k of every row (unscaled)
     float* mass;                 // steps with weights
+    int mass_inside;             // ... of whole units are accumulated by the CTA that has the unit
     int* status;
 };
 cudaError_t launch_chunk(const CUtensorMap& map_q, const CUtensorMap& map_k, const CUtensorMap& map_v, const ChunkParams& p,

@@ -211,6 +211,7 @@ int evict(const void* cache_k, const void* cache_v, const float* mass, const int
 
 // ---- attention of the newest tokens -----------------------------------------------------------------
 constexpr int kMaxCtas = 192;            // of a launch
+constexpr int kMassInside = 2048;        // rows of a cache
 
 // The workspace behind the status word: partial rows of the pieces (two a CTA), logits and log-sum-exps of a step.
 struct ChunkSpace { size_t parts, part_lse, logits, lse, total; };
@@ -342,9 +343,12 @@ int chunk_attention(const void* q, const void* cache_k, const void* cache_v, flo
         Batch<ChunkReq, kManyRequests> b;
         b.n = (int)std::min<size_t>(kManyRequests, reqs.size() - base);
         b.pad = 0;
+        b.r[0] = reqs[base];
         long long total = 0;
         const bool shares = takes_shares(&reqs[base], b.n, tile_tokens, heads, rows, sms, &total);
         int ctas = sms;
+        // Weights of short caches don't wait for a second launch.  (Of long ones half a CTA would take too long.)
+        p.mass_inside = step && b.r[0].len <= kMassInside;
         p.n_units = p.share = p.total_steps = 0;
         if (shares) {
             p.total_steps = (int)total;
@@ -363,7 +367,7 @@ int chunk_attention(const void* q, const void* cache_k, const void* cache_v, flo
         }
         LOOKM_CUDA(launch_chunk(map_q, map_k, map_v, p, b, std::min(ctas, shares ? ctas : p.n_units), st));
         ++g_launches;
-        if (shares || step) {
+        if (shares || (step && !p.mass_inside)) {
             LOOKM_CUDA(launch_chunk_finish(p, b, st));
             ++g_launches;
         }
