@@ -76,8 +76,12 @@ struct Walk {
     template <int kRequests>
     __device__ __forceinline__ void start(const ChunkParams& p, const Batch<ChunkReq, kRequests>& batch) {
         round = 0;
-        if (p.share == 0) return;
-        pos = blockIdx.x * p.share;
+        if (p.share > 0) find(blockIdx.x * p.share, p, batch);
+    }
+    // To step `at`.
+    template <int kRequests>
+    __device__ __forceinline__ void find(int at, const ChunkParams& p, const Batch<ChunkReq, kRequests>& batch) {
+        pos = at;
         int lo = 0, hi = batch.n - 1;
         while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
@@ -336,12 +340,10 @@ __device__ __forceinline__ void issue_mmas(const ChunkParams& p, const Batch<Chu
             if (it.nt == 1) queries_done();
             outputs_free();
             for (int t = 0; t < it.nt && !stop; ++t) {
-                const uint32_t v = arrived();
+                const uint32_t v = arrived();    // (both waits before those that matter: the tensor core's queue is short)
+                if (t + 1 < it.nt) k = arrived();
                 if (t < it.nt0) pv(0, v);
-                if (t + 1 < it.nt) {
-                    k = arrived();
-                    if (t + 1 < it.nt0) qk(0, k);
-                }
+                if (t + 1 < it.nt0) qk(0, k);
                 pv(1, v);
                 release(v);
                 if (t + 1 < it.nt) {
@@ -360,11 +362,12 @@ __device__ __forceinline__ void issue_mmas(const ChunkParams& p, const Batch<Chu
             outputs_free();
             for (int t = 0; t < it.nt && !stop; ++t) {
                 const uint32_t v = arrived();
+                uint32_t k = 0;
+                if (t + 2 < it.nt) k = arrived();
                 pv(t & 1, v);
+                if (t + 2 < it.nt) qk(t & 1, k);
                 release(v);
                 if (t + 2 < it.nt) {
-                    const uint32_t k = arrived();
-                    qk(t & 1, k);
                     release(k);
                     if (t + 3 == it.nt) queries_done();
                 }
@@ -677,6 +680,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     ChunkShared& sh = *reinterpret_cast<ChunkShared*>(smem_raw);
     if (ptx::smem_u32(smem_raw) & 1023u) {       // (the swizzle needs it, and there is no room to round up in)
+        grid_dependency_wait();
         if (threadIdx.x == 0) atomicMax(p.status, (int)LOOKM_ERR_UNSUPPORTED);
         return;
     }
@@ -743,83 +747,110 @@ constexpr int kMassRows = 4 * kFinishThreads;    // cached rows of a CTA
 // What a unit was cut into: CTAs first .. last, some of which may have none of its tiles.
 struct Cuts {
     ChunkUnit u;
-    int begin, first, last, pieces;
-    __device__ __forceinline__ Cuts(const ChunkParams& p, const ChunkReq& q, int head, int set) {
+    int begin, first, last;
+    __device__ __forceinline__ Cuts(const ChunkParams& p, const ChunkUnit& unit, int unit_begin) {
+        u = unit;
+        begin = unit_begin;
         first = last = 0;
-        pieces = 1;
-        u = chunk_unit(q, set, p.tile_tokens);
         if (p.share == 0) return;
-        begin = q.step_begin + head * q.head_steps;
-        for (int s = 0; s < set; ++s) begin += chunk_unit(q, s, p.tile_tokens).steps;
         first = begin / p.share;
         last = (begin + u.steps - 1) / p.share;
-        pieces = 0;
-        for (int c = first; c <= last; ++c) pieces += piece_of(p, c) >= 0;
     }
     // The piece that CTA c has; -1: none
     __device__ __forceinline__ int piece_of(const ChunkParams& p, int c) const {
         const int from = c * p.share - begin, to = from + p.share;
         if (chunk_cut(u, max(from, 0)) == chunk_cut(u, to)) return -1;
-        return 2 * c + (from >= 0 ? 0 : c == first ? 1 : 0);
+        return 2 * c + (from >= 0 ? 0 : 1);
+    }
+    // Whether the unit has several pieces: a whole one has left none.
+    __device__ __forceinline__ bool is_cut(const ChunkParams& p) const {
+        if (first == last) return false;
+        int pieces = 0;
+        for (int c = first; c <= last && pieces < 2; ++c) pieces += piece_of(p, c) >= 0;
+        return pieces > 1;
     }
 };
 
-// log2-sum-exp2 of a row of a unit that was cut; by a whole warp.
-__device__ __forceinline__ float row_lse2(const ChunkParams& p, const Cuts& cuts, int row, float& top) {
-    const int lane = threadIdx.x & 31;
-    top = -INFINITY;
-    for (int c = cuts.first + lane; c <= cuts.last; c += 32) {
+// log2-sum-exp2 of a row of a unit that was cut; by kLanes lanes side by side, all of them of a warp together.
+template <int kLanes>
+__device__ __forceinline__ float row_lse2(const ChunkParams& p, const Cuts& cuts, int row) {
+    const int lane = threadIdx.x & (kLanes - 1);
+    float top = -INFINITY, sum = 0.f;
+    for (int c = cuts.first + lane; c <= cuts.last; c += kLanes) {
         const int piece = cuts.piece_of(p, c);
         if (piece >= 0) top = fmaxf(top, p.part_lse[(long long)piece * p.slot_rows + row]);
     }
 #pragma unroll
-    for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+    for (int d = kLanes / 2; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
     if (top == -INFINITY) top = 0.f;
-    float sum = 0.f;
-    for (int c = cuts.first + lane; c <= cuts.last; c += 32) {
+    for (int c = cuts.first + lane; c <= cuts.last; c += kLanes) {
         const int piece = cuts.piece_of(p, c);
         if (piece >= 0) sum += ptx::ex2(p.part_lse[(long long)piece * p.slot_rows + row] - top);
     }
 #pragma unroll
-    for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    for (int d = kLanes / 2; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
     return top + ptx::lg2(sum);
 }
 
-// An output row of a unit that was cut, by a whole warp: the pieces' rows in order, each times 2^(its log-sum-exp - the row's).
+// An output row of a unit that was cut, by half a warp: the pieces' rows in order, each times 2^(its log-sum-exp - the row's).  Both halves come
+// here together, each with a row, which may be the same.
 __device__ __forceinline__ void add_pieces(const ChunkParams& p, const ChunkReq& q, const Cuts& cuts, int head, int row) {
-    const int lane = threadIdx.x & 31;
-    float top;
-    const float lse2 = row_lse2(p, cuts, row, top);
-    float4 acc = {0.f, 0.f, 0.f, 0.f};
-    for (int c0 = cuts.first; c0 <= cuts.last; c0 += 32) {
+    const int lane = threadIdx.x & 15;
+    const float lse2 = row_lse2<16>(p, cuts, row);
+    float acc[8] = {};
+    for (int c0 = cuts.first; c0 <= cuts.last; c0 += 16) {
         const int mine = c0 + lane <= cuts.last ? cuts.piece_of(p, c0 + lane) : -1;
         const float x = mine >= 0 ? p.part_lse[(long long)mine * p.slot_rows + row] : -INFINITY;
         const float w = x == -INFINITY ? 0.f : ptx::ex2(x - lse2);
-        const int n = min(32, cuts.last - c0 + 1);
-#pragma unroll 8
+        const int n = min(16, cuts.last - c0 + 1);
+#pragma unroll 4
         for (int i = 0; i < n; ++i) {
-            const int piece = __shfl_sync(0xffffffffu, mine, i);
-            const float wi = __shfl_sync(0xffffffffu, w, i), xi = __shfl_sync(0xffffffffu, x, i);
+            const int piece = __shfl_sync(0xffffffffu, mine, i, 16);
+            const float wi = __shfl_sync(0xffffffffu, w, i, 16), xi = __shfl_sync(0xffffffffu, x, i, 16);
             if (xi == -INFINITY) continue;
-            const float4 o = *reinterpret_cast<const float4*>(p.part_out + ((long long)piece * p.slot_rows + row) * kHeadDim + lane * 4);
-            acc.x = fmaf(o.x, wi, acc.x);
-            acc.y = fmaf(o.y, wi, acc.y);
-            acc.z = fmaf(o.z, wi, acc.z);
-            acc.w = fmaf(o.w, wi, acc.w);
+            const float4* o = reinterpret_cast<const float4*>(p.part_out + ((long long)piece * p.slot_rows + row) * kHeadDim + lane * 8);
+            const float4 o0 = o[0], o1 = o[1];
+            const float v[8] = {o0.x, o0.y, o0.z, o0.w, o1.x, o1.y, o1.z, o1.w};
+#pragma unroll
+            for (int k = 0; k < 8; ++k) acc[k] = fmaf(v[k], wi, acc[k]);
         }
+        __syncwarp();
     }
     const long long tok = q.q_begin + cuts.u.tok0 + row / p.group;
     const int q_head = head * p.group + row % p.group;
-    const float none = lse2 == -INFINITY ? NAN : 0.f;          // no row has a weight
-    *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.out) + (tok * p.pages.n_q_heads + q_head) * kHeadDim + lane * 4) =
-        make_uint2(pack_bf16(acc.x + none, acc.y + none), pack_bf16(acc.z + none, acc.w + none));
+    if (lse2 == -INFINITY) {                     // no row has a weight
+#pragma unroll
+        for (int k = 0; k < 8; ++k) acc[k] = NAN;
+    }
+    *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.out) + (tok * p.pages.n_q_heads + q_head) * kHeadDim + lane * 8) =
+        make_uint4(pack_bf16(acc[0], acc[1]), pack_bf16(acc[2], acc[3]), pack_bf16(acc[4], acc[5]), pack_bf16(acc[6], acc[7]));
     if (lane == 0 && p.lse) p.lse[(long long)q_head * p.n_tokens + tok] = lse2 * 0.6931471805599453f;
 }
+// ... all rows of the unit, `stride` half-warps from number `first` on
+__device__ __forceinline__ void add_pieces_of_rows(const ChunkParams& p, const ChunkReq& q, const Cuts& cuts, int head, int first, int stride) {
+    const int rows = min(q.n_new - cuts.u.tok0, 2 * p.tile_tokens) * p.group;
+    const int half = (threadIdx.x >> 4) & 1;
+    for (int row = first - half; row < rows; row += stride) add_pieces(p, q, cuts, head, min(row + half, rows - 1));
+}
 
-// blockIdx.x: unit; blockIdx.y: its rows in turn, or with weights blocks of cached rows (of which the first also has the rows).
-template <int kRequests, bool kStep>
-__global__ void __launch_bounds__(kFinishThreads, 4)
+// blockIdx.x: a place between two CTAs' shares, and so a unit that may have been cut there (its first such place has it);
+// blockIdx.y: rows in turn.
+template <int kRequests>
+__global__ void __launch_bounds__(kFinishThreads)
 chunk_finish_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__ Batch<ChunkReq, kRequests> batch) {
+    Walk at;
+    at.find((blockIdx.x + 1) * p.share, p, batch);
+    const ChunkReq& q = batch.r[at.r];
+    const Cuts cuts(p, chunk_unit(q, at.set, p.tile_tokens), at.begin);
+    grid_dependency_wait();                      // (also by CTAs that leave: this grid's end has to mean the end of the one before it)
+    if (cuts.first != (int)blockIdx.x || !cuts.is_cut(p)) return;
+    add_pieces_of_rows(p, q, cuts, at.head, blockIdx.y * (2 * kFinishWarps) + (threadIdx.x >> 4), gridDim.y * 2 * kFinishWarps);
+}
+
+// Steps with weights.  blockIdx.x: unit; blockIdx.y: a block of its cached rows (the first also has the output rows).
+template <int kRequests>
+__global__ void __launch_bounds__(kFinishThreads, 4)
+step_finish_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__ Batch<ChunkReq, kRequests> batch) {
     __shared__ float lse2[kTile];
     int lo = 0, hi = batch.n - 1;
     while (lo < hi) {
@@ -827,28 +858,21 @@ chunk_finish_kernel(const __grid_constant__ ChunkParams p, const __grid_constant
         if (batch.r[mid].unit_begin <= (int)blockIdx.x) lo = mid; else hi = mid - 1;
     }
     const ChunkReq& q = batch.r[lo];
-    const int k = blockIdx.x - q.unit_begin, head = k % p.pages.n_kv_heads, warp = threadIdx.x >> 5;
-    const Cuts cuts(p, q, head, k / p.pages.n_kv_heads);
-    grid_dependency_wait();                      // (also by CTAs that leave: this grid's end has to mean the end of the one before it)
-    if (kStep ? (long long)blockIdx.y * kMassRows >= q.len || (p.mass_inside && cuts.pieces == 1) : cuts.pieces == 1) return;
-    if (cuts.pieces > 1) {
-        const int rows = min(q.n_new - cuts.u.tok0, 2 * p.tile_tokens) * p.group;
-        if (!kStep || blockIdx.y == 0)
-            for (int row = (kStep ? 0 : blockIdx.y * kFinishWarps) + warp; row < rows; row += (kStep ? 1 : gridDim.y) * kFinishWarps)
-                add_pieces(p, q, cuts, head, row);
+    const int head = blockIdx.x - q.unit_begin, warp = threadIdx.x >> 5;
+    const Cuts cuts(p, chunk_unit(q, 0, p.tile_tokens), q.step_begin + head * q.head_steps);
+    grid_dependency_wait();
+    const bool is_cut = cuts.is_cut(p);
+    if ((long long)blockIdx.y * kMassRows >= q.len || (p.mass_inside && !is_cut)) return;
+    if (is_cut && blockIdx.y == 0) add_pieces_of_rows(p, q, cuts, head, threadIdx.x >> 4, 2 * kFinishWarps);
+    for (int g = warp; g < p.group; g += kFinishWarps) {
+        const float x = is_cut ? row_lse2<32>(p, cuts, g)
+                               : p.lse[(long long)(head * p.group + g) * p.n_tokens + q.q_begin] * 1.4426950408889634f;
+        if ((threadIdx.x & 31) == 0) lse2[g] = x;
     }
-    if constexpr (kStep) {
-        for (int g = warp; g < p.group; g += kFinishWarps) {
-            float top;
-            const float x = cuts.pieces > 1 ? row_lse2(p, cuts, g, top)
-                                            : p.lse[(long long)(head * p.group + g) * p.n_tokens + q.q_begin] * 1.4426950408889634f;
-            if ((threadIdx.x & 31) == 0) lse2[g] = x;
-        }
-        __syncthreads();
-        const int t0 = blockIdx.y * kMassRows;
-        add_weights(p, q.index, head, q.len, p.logits + q.logits_begin + (long long)head * p.group * q.len, lse2, t0 + threadIdx.x,
-                    min(q.len, t0 + kMassRows), kFinishThreads);
-    }
+    __syncthreads();
+    const int t0 = blockIdx.y * kMassRows;
+    add_weights(p, q.index, head, q.len, p.logits + q.logits_begin + (long long)head * p.group * q.len, lse2, t0 + threadIdx.x,
+                min(q.len, t0 + kMassRows), kFinishThreads);
 }
 
 template <int kRequests>
@@ -875,12 +899,15 @@ cudaError_t launch(const CUtensorMap& map_q, const CUtensorMap& map_k, const CUt
 
 template <int kRequests>
 cudaError_t finish(const ChunkParams& p, const Batch<ChunkReq, kManyRequests>& batch, cudaStream_t stream) {
-    int len = 0;
-    for (int i = 0; i < batch.n; ++i) len = std::max(len, batch.r[i].len);
-    if (p.mass)
-        return launch_chained(chunk_finish_kernel<kRequests, true>, dim3(p.n_units, (len + kMassRows - 1) / kMassRows), dim3(kFinishThreads), 0,
-                              stream, p, shorter<kRequests>(batch));
-    return launch_chained(chunk_finish_kernel<kRequests, false>, dim3(p.n_units, (p.slot_rows + kFinishWarps - 1) / kFinishWarps),
+    if (p.mass) {
+        int len = 0;
+        for (int i = 0; i < batch.n; ++i) len = std::max(len, batch.r[i].len);
+        return launch_chained(step_finish_kernel<kRequests>, dim3(p.n_units, (len + kMassRows - 1) / kMassRows), dim3(kFinishThreads), 0, stream,
+                              p, shorter<kRequests>(batch));
+    }
+    const int places = (p.total_steps - 1) / p.share;
+    if (places == 0) return cudaSuccess;
+    return launch_chained(chunk_finish_kernel<kRequests>, dim3(places, (p.slot_rows + 2 * kFinishWarps - 1) / (2 * kFinishWarps)),
                           dim3(kFinishThreads), 0, stream, p, shorter<kRequests>(batch));
 }
 

@@ -231,23 +231,29 @@ int slot_rows(const lookm_paged_layout* l, long long most_new) {
     return (int)std::min<long long>(2ll * (kTile / group) * group, std::max<long long>(most_new, 1) * group);
 }
 
-// Whether the CTAs of a launch take equal shares of all units' steps instead of whole units: where the longest of these
-// would keep its SM busy for longer than a share and a second launch.
+// Whether the CTAs of a launch take equal shares of all units' steps instead of whole units: where the SM with the most whole units
+// would be busy for longer than a share, a second launch and what the pieces' partial rows cost.  A step takes about
+// 1 us.  us, whole | shares: one prompt of 4096 tokens x 32 heads 131 | 163, 512 tokens over 32256, 32 heads on 8, 433 | 256, 8 x 256 over
+// 9000, 8 heads, 132 | 100, 16 x 128 over 9000, 32 on 8, 284 | 310, 100 over 5000 x 40 49 | 34, one over 2000 x 32 21.6 | 18.3, four
+// of one over 1000 to 3000 x 32 35.1 | 36.3.
 bool takes_shares(const ChunkReq* reqs, int n, int tile_tokens, int heads, int rows, int sms, long long* total) {
-    long long units = 0, steps = 0, longest = 0;
-    for (int r = 0; r < n; ++r) {
-        units += (long long)reqs[r].n_sets * heads;
-        if (units >= 4ll * sms) return false;
-        for (int s = 0; s < reqs[r].n_sets; ++s) {
+    long long units = 0, steps = 0;
+    for (int r = 0; r < n; ++r) units += (long long)reqs[r].n_sets * heads;
+    if (units >= 4ll * sms) return false;
+    long long load[kMaxCtas] = {}, most = 0;         // the kernel's own deal of whole units
+    int i = 0, step = 1;
+    for (int r = 0; r < n; ++r)
+        for (int s = reqs[r].n_sets - 1; s >= 0; --s) {
             const int k = chunk_unit(reqs[r], s, tile_tokens).steps;
             steps += (long long)k * heads;
-            longest = std::max<long long>(longest, k);
+            for (int h = 0; h < heads; ++h) {
+                most = std::max(most, load[i] += k);
+                i += step;
+                if (i == sms || i < 0) { i -= step; step = -step; }
+            }
         }
-    }
     *total = steps;
-    if (steps >= (1ll << 30)) return false;
-    const long long share = (steps + sms - 1) / sms, whole = units <= sms ? longest : std::max(longest, share + longest / 2);
-    return whole > share + 6 + rows / 16;
+    return steps < (1ll << 30) && most > (steps + sms - 1) / sms + 8 + rows / 8;
 }
 
 // bf16 [tokens, heads, 128]: boxes of the rows of a query tile
