@@ -256,9 +256,11 @@ int lookm_decode_step_varlen(const void* q, const void* k_new, const void* v_new
  * only read.
  *
  * The status word: these calls raise it and never clear it, so a problem stays reported until
- * lookm_device_status() has returned it.  Clear a workspace's first 256 bytes once before its first use.
+ * lookm_device_status() has returned it.  Clear a workspace's first 256 bytes before its first use here, and again if
+ * calls of another kind have used it in between.
  *
- * Query heads share KV heads as in lookm_layout; a group of more than 128 is LOOKM_ERR_UNSUPPORTED. */
+ * Query heads share KV heads as in lookm_layout; a group of more than 128, a cache of more than 2^25 rows and a call of
+ * more than 2^25 tokens are LOOKM_ERR_UNSUPPORTED. */
 typedef struct {
     int n_q_heads, n_kv_heads, head_dim;
     int page_rows, n_pages, table_stride;

@@ -373,9 +373,12 @@ def make_paged_layout(q, cache_k, page_table, softmax_scale: float = 0.0, n_q_he
     """Layout of a pool seen as [n_pages, n_kv_heads, page_rows, 128] (any strides, last dim contiguous), a table
     [n_requests, table_stride] and queries [T, Hq, 128].  q may be None (lookm_evict, or a workspace's size) if n_q_heads is given."""
     assert cache_k.stride(3) == 1 and page_table.stride(1) == 1 and (q is None or q.stride(2) == 1)
-    hq, st, sh = (n_q_heads, 0, 0) if q is None else (q.shape[1], q.stride(0), q.stride(1))
-    # (a dimension of one has any stride: the least that is allowed will do)
-    stride = lambda d: cache_k.stride(d) if cache_k.shape[d] > 1 else max(cache_k.stride(d), 128)
+    # (a dimension of one may have any stride: one that is allowed will do)
+    hq, st, sh = n_q_heads, 0, 0
+    if q is not None:
+        hq, sh = q.shape[1], q.stride(1) if q.shape[1] > 1 else 128
+        st = q.stride(0) if q.shape[0] > 1 else hq * sh
+    stride = lambda d: cache_k.stride(d) if cache_k.shape[d] > 1 else 128
     table_stride = page_table.stride(0) if page_table.shape[0] > 1 else page_table.shape[1]
     return PagedLayout(hq, cache_k.shape[1], cache_k.shape[3], cache_k.shape[2], cache_k.shape[0], table_stride, stride(0), stride(2),
                        stride(1), st, sh, float(softmax_scale))

@@ -11,7 +11,7 @@
 namespace lookm {
 namespace {
 
-constexpr int kMaxLen = 1 << 30;         // rows of a cache
+constexpr int kMaxLen = 1 << 25;         // rows of a cache, tokens of a call
 
 bool aligned(const void* p, unsigned bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 
@@ -35,7 +35,8 @@ int check_requests(const lookm_paged_layout* l, int n, const int* lens) {
     if (n > 65535) return LOOKM_ERR_UNSUPPORTED;
     long long total = 0;
     for (int r = 0; r < n; ++r) {
-        if (lens[r] < 0 || lens[r] > kMaxLen) return LOOKM_ERR_INVALID_ARG;
+        if (lens[r] < 0) return LOOKM_ERR_INVALID_ARG;
+        if (lens[r] > kMaxLen) return LOOKM_ERR_UNSUPPORTED;
         if (((long long)lens[r] + l->page_rows - 1) / l->page_rows > l->table_stride) return LOOKM_ERR_INVALID_ARG;
         total += lens[r];
     }
@@ -98,7 +99,8 @@ int append_rows(const void* q, const void* k, const void* v, const int* position
     LOOKM_TRY(check_requests(paged, n, lens));
     for (int r = 0; r < n; ++r) {
         const long long len = (long long)lens[r] + cu[r + 1] - cu[r];
-        if (len > kMaxLen || (len + paged->page_rows - 1) / paged->page_rows > paged->table_stride) return LOOKM_ERR_INVALID_ARG;
+        if (len > kMaxLen) return LOOKM_ERR_UNSUPPORTED;
+        if ((len + paged->page_rows - 1) / paged->page_rows > paged->table_stride) return LOOKM_ERR_INVALID_ARG;
     }
     LOOKM_TRY(check_pool(cache_k, cache_v, table));
     for (const void* p : {q, k, v, (const void*)q_out})
