@@ -171,54 +171,61 @@ evict_copy_kernel(const EvictParams p, const __grid_constant__ Batch<EvictReq, k
     }
 }
 
-// In place.  A CTA takes a slice of 1 / kSlices of the features of all kept rows of one pool's head, in ascending order and a
-// batch at a time: all loads of a batch, a barrier, its stores.  Row i comes from row kept[i] >= i, so a store never
-// hits a row that a later batch still reads, and other CTAs touch other bytes.
-// The next batch's rows are asked for before this one's are stored.
+// In place.  A cluster of CTAs takes a slice of 1 / kSlices of the features of all kept rows of one pool's head, in ascending order and
+// a batch at a time: all loads of a batch, a barrier, its stores.  Row i comes from row kept[i] >= i, so a store never hits a row
+// that a later batch still reads, and other clusters touch other bytes.  The rows of the next batch are asked for before this one's are
+// stored, their numbers and pages a batch earlier still.
 constexpr int kPlaceRows = 4;                    // of a thread at a time
 template <int kSlices, int kRequests>
 __global__ void __launch_bounds__(kMoveThreads)
-evict_in_place_kernel(const EvictParams p, const __grid_constant__ Batch<EvictReq, kRequests> batch) {
-    constexpr int kLanes = 16 / kSlices, kGroups = kMoveThreads / kLanes, kStep = kGroups * kPlaceRows;   // lanes of a row, rows side by side
+evict_in_place_kernel(const EvictParams p, const __grid_constant__ Batch<EvictReq, kRequests> batch, int cluster) {
+    constexpr int kLanes = 16 / kSlices, kGroups = kMoveThreads / kLanes;        // lanes of a row, rows side by side
+    const int unit = blockIdx.x / cluster, part = blockIdx.x % cluster, group = part * kGroups + threadIdx.x / kLanes;
+    const int side = kGroups * cluster, step = side * kPlaceRows;
     const EvictReq& rq = batch.r[blockIdx.z];
-    const int h = blockIdx.y, slice = blockIdx.x >> 1;
-    const bool is_v = blockIdx.x & 1, has_mass = blockIdx.x == 0 && threadIdx.x % kLanes == 0;
+    const int h = blockIdx.y, slice = unit >> 1;
+    const bool is_v = unit & 1, has_mass = unit == 0 && threadIdx.x % kLanes == 0;
     grid_dependency_wait();
     const int* kept = p.kept + rq.kept_off + (long long)h * rq.budget;
     Pages out = p.pages;
     out.table = p.out_table;
     const char* in = static_cast<const char*>(is_v ? p.cache_v : p.cache_k) + (slice * kLanes + threadIdx.x % kLanes) * 16;
     char* to_pool = static_cast<char*>(is_v ? p.out_v : p.out_k) + (slice * kLanes + threadIdx.x % kLanes) * 16;
+    int from[kPlaceRows], src[kPlaceRows];       // of the batch whose rows are asked for next; src < 0: none
+    const auto find = [&](int base) {
+#pragma unroll
+        for (int j = 0; j < kPlaceRows; ++j) {
+            const int i = base + j * side + group;
+            from[j] = i < rq.budget ? kept[i] : -1;
+        }
+#pragma unroll
+        for (int j = 0; j < kPlaceRows; ++j) src[j] = from[j] < 0 ? -1 : p.pages.page_of(rq.index, from[j], p.status);
+    };
     struct Rows {
         uint4 x[kPlaceRows];
         float m[kPlaceRows];
         int page[kPlaceRows];                    // where they go; -1: nowhere
     } now, next;
     const auto ask = [&](int base, Rows& b) {
-        int from[kPlaceRows];
-#pragma unroll
-        for (int j = 0; j < kPlaceRows; ++j) {
-            const int i = base + j * kGroups + threadIdx.x / kLanes;
-            from[j] = i < rq.budget ? kept[i] : -1;
-        }
 #pragma unroll
         for (int j = 0; j < kPlaceRows; ++j) {
             b.page[j] = -1;
-            if (from[j] < 0) continue;
-            const int src = p.pages.page_of(rq.index, from[j], p.status);
-            if (src < 0) continue;
-            b.page[j] = out.page_of(rq.index, base + j * kGroups + threadIdx.x / kLanes, p.status);
-            b.x[j] = *reinterpret_cast<const uint4*>(in + 2 * p.pages.row_at(src, from[j], h));
-            if (has_mass) b.m[j] = p.mass[p.pages.mass_at(src, from[j], h)];
+            if (src[j] < 0) continue;
+            b.x[j] = *reinterpret_cast<const uint4*>(in + 2 * p.pages.row_at(src[j], from[j], h));
+            if (has_mass) b.m[j] = p.mass[p.pages.mass_at(src[j], from[j], h)];
+            b.page[j] = out.page_of(rq.index, base + j * side + group, p.status);
         }
     };
+    find(0);
     ask(0, now);
-    for (int base = 0; base < rq.budget; base += kStep) {
-        if (base + kStep < rq.budget) ask(base + kStep, next);
-        __syncthreads();
+    find(step);
+    for (int base = 0; base < rq.budget; base += step) {
+        ask(base + step, next);
+        find(base + 2 * step);
+        if (cluster > 1) ptx::cluster_sync(); else __syncthreads();
 #pragma unroll
         for (int j = 0; j < kPlaceRows; ++j) {
-            const int i = base + j * kGroups + threadIdx.x / kLanes;
+            const int i = base + j * side + group;
             if (now.page[j] < 0) continue;
             *reinterpret_cast<uint4*>(to_pool + 2 * out.row_at(now.page[j], i, h)) = now.x[j];
             if (has_mass) p.out_mass[out.mass_at(now.page[j], i, h)] = now.m[j];
@@ -248,13 +255,16 @@ cudaError_t launch(const EvictParams& p, const Batch<EvictReq, kManyRequests>& b
     if (err != cudaSuccess) return err;
     ++*launches;
     if (in_place) {
-        // slices: as many as give every SM a CTA or two
-        const long long units = 2ll * heads * b.n;
-        const int slices = units * 2 >= num_sms * 2 ? 2 : units * 4 >= num_sms * 2 ? 4 : 8;
-        const auto move = slices == 2   ? evict_in_place_kernel<2, kRequests>
-                          : slices == 4 ? evict_in_place_kernel<4, kRequests>
-                                        : evict_in_place_kernel<8, kRequests>;
-        err = launch_chained(move, dim3(2 * slices, heads, b.n), dim3(kMoveThreads), 0, stream, p, b);
+        // Few units (pools x heads x requests): slices and clusters until every SM has some CTAs, as long as a batch does not exceed
+        // the rows.
+        const long long units = 2ll * heads * b.n, want = 4ll * num_sms;
+        const int slices = units * 2 >= want ? 2 : 4;
+        int cluster = 1;
+        while (cluster < 8 && units * slices * cluster * 2 <= want + want / 4 &&
+               cluster * 2 * kPlaceRows * kMoveThreads * slices / 16 <= budget)
+            cluster *= 2;
+        const auto move = slices == 2 ? evict_in_place_kernel<2, kRequests> : evict_in_place_kernel<4, kRequests>;
+        err = launch_chained_clusters(move, dim3(2 * slices * cluster, heads, b.n), dim3(kMoveThreads), cluster, 0, stream, p, b, cluster);
     } else {
         constexpr int kRows = kMoveThreads / 16 * kMoveRows;
         err = launch_chained(evict_copy_kernel<kRequests>, dim3((budget + kRows - 1) / kRows, heads, b.n), dim3(kMoveThreads), 0, stream,

@@ -191,8 +191,7 @@ int evict(const void* cache_k, const void* cache_v, const float* mass, const int
     p.kept = kept ? kept : at<int>(ws, kStatusBytes);
     p.status = at<int>(ws, 0);
     const bool in_place = cache_k == out_k || cache_v == out_v || mass == out_mass;
-    Batch<EvictReq, kManyRequests> b;
-    b.n = b.pad = 0;
+    std::vector<EvictReq> reqs;
     long long off = 0;
     for (int r = 0; r < n; ++r) {
         EvictReq q;
@@ -202,11 +201,16 @@ int evict(const void* cache_k, const void* cache_v, const float* mass, const int
         q.index = r;
         q.kept_off = off;
         off += (long long)q.budget * paged->n_kv_heads;
-        if (q.budget > 0) b.r[b.n++] = q;
-        if (b.n == kManyRequests || (r == n - 1 && b.n)) {
-            LOOKM_CUDA(launch_evict(p, b, in_place, di.sms, static_cast<cudaStream_t>(stream), &g_launches));
-            b.n = 0;
-        }
+        if (q.budget > 0) reqs.push_back(q);
+    }
+    // the longest first, so that none of them is left for the end
+    std::stable_sort(reqs.begin(), reqs.end(), [](const EvictReq& a, const EvictReq& b) { return a.budget > b.budget; });
+    for (size_t base = 0; base < reqs.size(); base += kManyRequests) {
+        Batch<EvictReq, kManyRequests> b;
+        b.n = (int)std::min<size_t>(kManyRequests, reqs.size() - base);
+        b.pad = 0;
+        for (int i = 0; i < b.n; ++i) b.r[i] = reqs[base + i];
+        LOOKM_CUDA(launch_evict(p, b, in_place, di.sms, static_cast<cudaStream_t>(stream), &g_launches));
     }
     return LOOKM_OK;
 }
