@@ -20,9 +20,9 @@
 namespace lookm {
 namespace {
 
-constexpr int kThreads = 256, kHalfWarps = kThreads / 16;
+constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kTokens = 4;                       // of a CTA, at most
-constexpr int kRows = 4;                         // of a half-warp at a time
+constexpr int kRows = 4, kUnitRows = 2 * kRows;  // of a half-warp at a time, of a warp
 
 struct TokenPlace { int index, row; };           // request and cache row
 
@@ -44,7 +44,7 @@ __device__ __forceinline__ uint32_t pack_bf16(ptx::f32x2 x) {
 // What a lane does to its features of every row of a token.
 struct Rotation {
     bool turned, adjacent;       // whether its features are rotated; pairs are neighbours
-    ptx::f32x2 cos[4], sin[4];   // adjacent: per pair, sin as (-sin, sin); else of the two pairs of the first group
+    ptx::f32x2 cos[4], sin[4], minus_sin[2];     // adjacent: per pair, sin as (-sin, sin); else of the two pairs of the first group
 };
 __device__ __forceinline__ void norm_rotate(Eight& e, bool norm, const Eight& weight, float eps, const Rotation& r) {
     if (norm) {
@@ -60,63 +60,68 @@ __device__ __forceinline__ void norm_rotate(Eight& e, bool norm, const Eight& we
 #pragma unroll
         for (int i = 0; i < 4; ++i) e.x[i] = ptx::mul2(ptx::mul2(e.x[i], scale2), weight.x[i]);
     }
-    if (!r.turned) return;
-    if (r.adjacent) {
+    if (r.turned) {
+        if (r.adjacent) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float2 v = ptx::unpack2(e.x[i]);
-            e.x[i] = ptx::fma2(e.x[i], r.cos[i], ptx::mul2(ptx::pack2(v.y, v.x), r.sin[i]));
-        }
-    } else {
-        const ptx::f32x2 minus = ptx::pack2(-1.f, -1.f);
+            for (int i = 0; i < 4; ++i) {
+                const float2 v = ptx::unpack2(e.x[i]);
+                e.x[i] = ptx::fma2(e.x[i], r.cos[i], ptx::mul2(ptx::pack2(v.y, v.x), r.sin[i]));
+            }
+        } else {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const ptx::f32x2 a = e.x[i], b = e.x[i + 2];
-            e.x[i] = ptx::fma2(a, r.cos[i], ptx::mul2(ptx::mul2(b, r.sin[i]), minus));
-            e.x[i + 2] = ptx::fma2(b, r.cos[i], ptx::mul2(a, r.sin[i]));
+            for (int i = 0; i < 2; ++i) {
+                const ptx::f32x2 a = e.x[i], b = e.x[i + 2];
+                e.x[i] = ptx::fma2(a, r.cos[i], ptx::mul2(b, r.minus_sin[i]));
+                e.x[i + 2] = ptx::fma2(b, r.cos[i], ptx::mul2(a, r.sin[i]));
+            }
         }
     }
+    __syncwarp();                                // (lanes that are not rotated have skipped that)
 }
 
-// Rows first .. last - 1 of a kind (queries, keys or values) of one token; all threads of the CTA.  kRows of a half-warp at a time, all
-// asked for together.  Both halves of a warp run the same number of rounds: they shuffle together.
-template <bool kWork>
-__device__ __forceinline__ void token_rows(const char* from, long long from_stride, char* to, long long to_stride, int first, int last, int at_a,
-                                           int at_b, bool norm, const Eight& weight, float eps, const Rotation& r) {
+// A warp's unit of work: up to 2 * kRows rows of one kind (queries, keys or values) of one token, half a warp each and all asked for
+// together.  `n` of them are there; src and dst are the lane's first group of four features in its half's first row.
+// kSplit: a lane's second group of four features does not follow its first but lies `gap` bytes on.
+template <bool kWork, bool kSplit>
+__device__ __forceinline__ void unit_rows(const char* src, long long from_stride, char* dst, long long to_stride, int n, int gap, bool norm,
+                                          const Eight& weight, float eps, const Rotation& r) {
     const int half = (threadIdx.x >> 4) & 1;
-    for (int i0 = first + (threadIdx.x >> 5) * 2; i0 < last; i0 += kHalfWarps * kRows) {
-        uint2 a[kRows], b[kRows];
+    uint2 a[kRows], b[kRows];
 #pragma unroll
-        for (int j = 0; j < kRows; ++j) {
-            const int i = i0 + j * kHalfWarps + half;
-            a[j] = b[j] = make_uint2(0, 0);
-            if (i < last) {
-                a[j] = *reinterpret_cast<const uint2*>(from + i * from_stride + at_a);
-                b[j] = *reinterpret_cast<const uint2*>(from + i * from_stride + at_b);
-            }
+    for (int j = 0; j < kRows; ++j, src += from_stride) {
+        a[j] = b[j] = make_uint2(0, 0);
+        if (2 * j + half >= n) continue;
+        if (kSplit) {
+            a[j] = *reinterpret_cast<const uint2*>(src);
+            b[j] = *reinterpret_cast<const uint2*>(src + gap);
+        } else {
+            const uint4 x = *reinterpret_cast<const uint4*>(src);
+            a[j] = make_uint2(x.x, x.y);
+            b[j] = make_uint2(x.z, x.w);
         }
+    }
 #pragma unroll
-        for (int j = 0; j < kRows; ++j) {
-            const int i = i0 + j * kHalfWarps + half;
-            if (i0 + j * kHalfWarps >= last) break;
-            if (kWork && (norm || r.turned)) {
-                Eight e = unpack8(a[j], b[j]);
-                norm_rotate(e, norm, weight, eps, r);
-                a[j] = make_uint2(pack_bf16(e.x[0]), pack_bf16(e.x[1]));
-                b[j] = make_uint2(pack_bf16(e.x[2]), pack_bf16(e.x[3]));
-            }
-            if (kWork) __syncwarp();             // (lanes that are not rotated may have skipped)
-            if (i < last) {
-                *reinterpret_cast<uint2*>(to + i * to_stride + at_a) = a[j];
-                *reinterpret_cast<uint2*>(to + i * to_stride + at_b) = b[j];
-            }
+    for (int j = 0; j < kRows; ++j, dst += to_stride) {
+        if (2 * j >= n) break;                   // (the same in both halves, which shuffle together)
+        if (kWork) {
+            Eight e = unpack8(a[j], b[j]);
+            norm_rotate(e, norm, weight, eps, r);
+            a[j] = make_uint2(pack_bf16(e.x[0]), pack_bf16(e.x[1]));
+            b[j] = make_uint2(pack_bf16(e.x[2]), pack_bf16(e.x[3]));
+        }
+        if (2 * j + half >= n) continue;
+        if (kSplit) {
+            *reinterpret_cast<uint2*>(dst) = a[j];
+            *reinterpret_cast<uint2*>(dst + gap) = b[j];
+        } else {
+            *reinterpret_cast<uint4*>(dst) = make_uint4(a[j].x, a[j].y, b[j].x, b[j].y);
         }
     }
 }
 
 template <int kRequests>
 __global__ void __launch_bounds__(kThreads, 4)
-append_kernel(const AppendParams p, const __grid_constant__ Batch<AppendReq, kRequests> batch, int tokens, int rows_per_cta) {
+append_kernel(const __grid_constant__ AppendParams p, const __grid_constant__ Batch<AppendReq, kRequests> batch, int tokens) {
     __shared__ float2 turn[kTokens][kMaxFreqs];
     __shared__ TokenPlace place[kTokens];
     const int t0 = p.tok_begin + blockIdx.x * tokens, nt = min(tokens, p.tok_end - t0);
@@ -139,21 +144,36 @@ append_kernel(const AppendParams p, const __grid_constant__ Batch<AppendReq, kRe
     }
     __syncthreads();
     const int hq = p.q ? p.pages.n_q_heads : 0, hkv = p.pages.n_kv_heads;
-    const int per_token = hq + 2 * hkv, first = blockIdx.y * rows_per_cta, last = min(first + rows_per_cta, per_token);
-    const int l = threadIdx.x & 15;
+    const int q_units = (hq + kUnitRows - 1) / kUnitRows, kv_units = (hkv + kUnitRows - 1) / kUnitRows, per_token = q_units + 2 * kv_units;
+    const int l = threadIdx.x & 15, half = (threadIdx.x >> 4) & 1;
     Rotation r;
     r.turned = l * 8 < p.rotary_dim;
     r.adjacent = p.interleaved;
-    const bool split = r.turned && !p.interleaved;             // first group 4 l .. 4 l + 3, second group half a rotation further
-    const int at_a = 2 * (split ? 4 * l : 8 * l), at_b = 2 * (split ? 4 * l + (p.rotary_dim >> 1) : 8 * l + 4);
-    const auto weight_of = [&](const void* w) {
-        const char* c = static_cast<const char*>(w);
-        return c ? unpack8(__ldg(reinterpret_cast<const uint2*>(c + at_a)), __ldg(reinterpret_cast<const uint2*>(c + at_b))) : Eight{};
-    };
-    const Eight wq = weight_of(p.q_weight), wk = weight_of(p.k_weight);
-    for (int t = 0; t < nt; ++t) {
-        const TokenPlace at = place[t];
+    // first group 4 l .. 4 l + 3, second group half a rotation further; else eight features in a row
+    const bool split = r.turned && !p.interleaved;
+    const int at = 2 * (split ? 4 * l : 8 * l), gap = split ? p.rotary_dim : 8;
+    for (int u = blockIdx.y * kWarps + (threadIdx.x >> 5); u < nt * per_token; u += gridDim.y * kWarps) {
+        const int t = u / per_token, k = u - t * per_token;
         const long long tok = t0 + t;
+        const TokenPlace to = place[t];
+        const bool is_q = k < q_units, is_k = !is_q && k < q_units + kv_units;
+        const int first = (k - (is_q ? 0 : is_k ? q_units : q_units + kv_units)) * kUnitRows, n = min(kUnitRows, (is_q ? hq : hkv) - first);
+        const long long from_stride = 2 * (is_q ? p.q_stride_head : p.kv_stride_head);
+        const long long to_stride = 2 * (is_q ? p.qo_stride_head : p.pages.head_stride);
+        const char* src = static_cast<const char*>(is_q ? p.q : is_k ? p.k : p.v) + 2 * tok * (is_q ? p.q_stride_tok : p.kv_stride_tok) +
+                          (first + half) * from_stride;
+        char* dst = static_cast<char*>(p.q_out) + 2 * tok * p.qo_stride_tok;
+        if (!is_q) {
+            const int page = p.pages.page_of(to.index, to.row, p.status);
+            if (page < 0) continue;
+            dst = static_cast<char*>(is_k ? p.cache_k : p.cache_v) + 2 * p.pages.row_at(page, to.row, 0);
+            if (is_k && p.mass && (threadIdx.x & 31) < n) p.mass[p.pages.mass_at(page, to.row, first + (threadIdx.x & 31))] = 0.f;
+        }
+        dst += (first + half) * to_stride;
+        const void* w = is_q ? p.q_weight : is_k ? p.k_weight : nullptr;
+        Eight weight{};
+        if (w) weight = unpack8(__ldg(reinterpret_cast<const uint2*>(static_cast<const char*>(w) + at)),
+                                __ldg(reinterpret_cast<const uint2*>(static_cast<const char*>(w) + at + gap)));
         if (r.turned) {
             const float2* angle = &turn[t][l * 4];
 #pragma unroll
@@ -164,27 +184,17 @@ append_kernel(const AppendParams p, const __grid_constant__ Batch<AppendReq, kRe
                 } else if (i < 2) {
                     r.cos[i] = ptx::pack2(angle[2 * i].x, angle[2 * i + 1].x);
                     r.sin[i] = ptx::pack2(angle[2 * i].y, angle[2 * i + 1].y);
+                    r.minus_sin[i] = ptx::pack2(-angle[2 * i].y, -angle[2 * i + 1].y);
                 }
             }
         }
         __syncwarp();
-        if (first < hq)
-            token_rows<true>(static_cast<const char*>(p.q) + 2 * tok * p.q_stride_tok, 2 * p.q_stride_head,
-                             static_cast<char*>(p.q_out) + 2 * tok * p.qo_stride_tok, 2 * p.qo_stride_head, first, min(last, hq), at_a, at_b,
-                             p.q_weight != nullptr, wq, p.eps, r);
-        const int page = p.pages.page_of(at.index, at.row, p.status);
-        if (page < 0) continue;
-        const long long row = 2 * p.pages.row_at(page, at.row, 0), from = 2 * tok * p.kv_stride_tok;
-        const int k0 = max(first - hq, 0), k1 = min(last - hq, hkv), v0 = max(first - hq - hkv, 0), v1 = last - hq - hkv;
-        if (k0 < k1) {
-            token_rows<true>(static_cast<const char*>(p.k) + from, 2 * p.kv_stride_head, static_cast<char*>(p.cache_k) + row,
-                             2 * p.pages.head_stride, k0, k1, at_a, at_b, p.k_weight != nullptr, wk, p.eps, r);
-            if (p.mass)
-                for (int h = k0 + threadIdx.x; h < k1; h += kThreads) p.mass[p.pages.mass_at(page, at.row, h)] = 0.f;
-        }
-        if (v0 < v1)
-            token_rows<false>(static_cast<const char*>(p.v) + from, 2 * p.kv_stride_head, static_cast<char*>(p.cache_v) + row,
-                              2 * p.pages.head_stride, v0, v1, 16 * l, 16 * l + 8, false, wk, 0.f, r);
+        if (!(is_q || is_k) || (!w && p.rotary_dim == 0))
+            unit_rows<false, false>(src + 16 * l, 2 * from_stride, dst + 16 * l, 2 * to_stride, n, 8, false, weight, 0.f, r);
+        else if (p.rotary_dim == 0 || p.interleaved)
+            unit_rows<true, false>(src + at, 2 * from_stride, dst + at, 2 * to_stride, n, gap, w != nullptr, weight, p.eps, r);
+        else
+            unit_rows<true, true>(src + at, 2 * from_stride, dst + at, 2 * to_stride, n, gap, w != nullptr, weight, p.eps, r);
     }
 }
 
@@ -194,13 +204,12 @@ cudaError_t launch(const AppendParams& p, const Batch<AppendReq, kManyRequests>&
     b.n = batch.n;
     b.pad = 0;
     for (int i = 0; i < kRequests; ++i) b.r[i] = i < batch.n ? batch.r[i] : AppendReq{0, 0, 0, 0};
-    const int total = p.tok_end - p.tok_begin, per_token = (p.q ? p.pages.n_q_heads : 0) + 2 * p.pages.n_kv_heads;
+    const int total = p.tok_end - p.tok_begin, hq = p.q ? p.pages.n_q_heads : 0;
+    const int units = (hq + kUnitRows - 1) / kUnitRows + 2 * ((p.pages.n_kv_heads + kUnitRows - 1) / kUnitRows);
     const int tokens = total >= kTokens * num_sms * 8 ? kTokens : 1, groups = (total + tokens - 1) / tokens;
-    // few tokens: a token's rows are spread over CTAs, down to one row per half-warp
-    const int parts = std::max(1, std::min((per_token + kHalfWarps - 1) / kHalfWarps, num_sms * 4 / groups));
-    const int rows = ((per_token + parts - 1) / parts + 1) / 2 * 2;
-    const dim3 grid(groups, (per_token + rows - 1) / rows);
-    return launch_chained(append_kernel<kRequests>, grid, dim3(kThreads), 0, stream, p, b, tokens, rows);
+    // few tokens: a token's units are spread over CTAs, down to one per warp
+    const int parts = std::max(1, std::min((units + kWarps - 1) / kWarps, num_sms * 4 / groups));
+    return launch_chained(append_kernel<kRequests>, dim3(groups, parts), dim3(kThreads), 0, stream, p, b, tokens);
 }
 
 }  // namespace
