@@ -430,23 +430,41 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     return *reinterpret_cast<const uint32_t*>(&ab);
 }
 
-// Steps: adds the weights of cached rows t, t + stride, ... < end to their mass, summed over the heads of the group; four rows at a time.
+// Steps: adds the weights of cached rows t, t + stride, ... < end to their mass, summed over the heads of the group; four rows at a time,
+// pages, logits of two heads and masses asked for together.
 __device__ __forceinline__ void add_weights(const ChunkParams& p, int index, int head, int len, const float* logits, const float* lse2, int t,
                                             int end, int stride) {
     for (; t < end; t += 4 * stride) {
         int page[4];
-        float w[4] = {0.f, 0.f, 0.f, 0.f}, m[4];
+        float w[4] = {0.f, 0.f, 0.f, 0.f}, m[4], x[2][4];
+        const auto ask = [&](int g, float (&y)[4]) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) page[j] = t + j * stride < end ? p.pages.page_of(index, t + j * stride, p.status) : -1;
-        for (int g = 0; g < p.group; ++g) {
-            float x[4];
+            for (int j = 0; j < 4; ++j) y[j] = t + j * stride < end ? logits[(long long)g * len + t + j * stride] : 0.f;
+        };
+        const auto add = [&](int g, const float (&y)[4]) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) x[j] = page[j] >= 0 ? logits[(long long)g * len + t + j * stride] : 0.f;
+            for (int j = 0; j < 4; ++j) w[j] += ptx::ex2(fmaf(y[j], p.scale_log2, -lse2[g]));
+        };
 #pragma unroll
-            for (int j = 0; j < 4; ++j) w[j] += ptx::ex2(fmaf(x[j], p.scale_log2, -lse2[g]));
+        for (int j = 0; j < 4; ++j)
+            page[j] = t + j * stride < end ? __ldg(p.pages.table + (long long)index * p.pages.table_stride + ((t + j * stride) >> p.pages.page_shift)) : 0;
+        ask(0, x[0]);
+        if (p.group > 1) ask(1, x[1]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (page[j] < 0 || page[j] >= p.pages.n_pages) {
+                atomicMax(p.status, (int)LOOKM_ERR_DEVICE_BAD_INDEX);
+                page[j] = -1;
+            }
+            if (t + j * stride >= end) page[j] = -1;
+            m[j] = page[j] >= 0 ? p.mass[p.pages.mass_at(page[j], t + j * stride, head)] : 0.f;
         }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) m[j] = page[j] >= 0 ? p.mass[p.pages.mass_at(page[j], t + j * stride, head)] : 0.f;
+        for (int g = 0; g < p.group; g += 2) {
+            add(g, x[0]);
+            if (g + 2 < p.group) ask(g + 2, x[0]);
+            if (g + 1 < p.group) add(g + 1, x[1]);
+            if (g + 3 < p.group) ask(g + 3, x[1]);
+        }
 #pragma unroll
         for (int j = 0; j < 4; ++j)
             if (page[j] >= 0) p.mass[p.pages.mass_at(page[j], t + j * stride, head)] = m[j] + w[j];
