@@ -898,7 +898,7 @@ Batch<ChunkReq, kRequests> shorter(const Batch<ChunkReq, kManyRequests>& batch) 
     Batch<ChunkReq, kRequests> b;
     b.n = batch.n;
     b.pad = 0;
-    for (int i = 0; i < kRequests; ++i) b.r[i] = i < batch.n ? batch.r[i] : ChunkReq{0, 0, 0, 0, 0, 0, 0, 1, 0};
+    for (int i = 0; i < kRequests; ++i) b.r[i] = i < batch.n ? batch.r[i] : ChunkReq{};
     return b;
 }
 
@@ -933,16 +933,16 @@ cudaError_t finish(const ChunkParams& p, const Batch<ChunkReq, kManyRequests>& b
 
 cudaError_t launch_chunk(const CUtensorMap& map_q, const CUtensorMap& map_k, const CUtensorMap& map_v, const ChunkParams& p,
                          const Batch<ChunkReq, kManyRequests>& batch, int grid, cudaStream_t stream) {
-    const bool few = batch.n <= kFewRequests;
+    const bool few = batch.n <= kFewChunks;
     if (p.logits)
-        return few ? launch<kFewRequests, true>(map_q, map_k, map_v, p, batch, grid, stream)
+        return few ? launch<kFewChunks, true>(map_q, map_k, map_v, p, batch, grid, stream)
                    : launch<kManyRequests, true>(map_q, map_k, map_v, p, batch, grid, stream);
-    return few ? launch<kFewRequests, false>(map_q, map_k, map_v, p, batch, grid, stream)
+    return few ? launch<kFewChunks, false>(map_q, map_k, map_v, p, batch, grid, stream)
                : launch<kManyRequests, false>(map_q, map_k, map_v, p, batch, grid, stream);
 }
 
 cudaError_t launch_chunk_finish(const ChunkParams& p, const Batch<ChunkReq, kManyRequests>& batch, cudaStream_t stream) {
-    return batch.n <= kFewRequests ? finish<kFewRequests>(p, batch, stream) : finish<kManyRequests>(p, batch, stream);
+    return batch.n <= kFewChunks ? finish<kFewChunks>(p, batch, stream) : finish<kManyRequests>(p, batch, stream);
 }
 
 }  // namespace lookm

@@ -31,8 +31,8 @@ struct Pages {
 };
 
 // The requests of a launch, by value (no table in device memory, no copy that would synchronise the host).  A launch takes
-// kFewRequests or kManyRequests of them; longer batches take several launches.
-constexpr int kFewRequests = 16, kManyRequests = 128;
+// kFewRequests (kFewChunks) or kManyRequests of them; longer batches take several launches.
+constexpr int kFewRequests = 16, kManyRequests = 128, kFewChunks = 32;
 template <class R, int kRequests>
 struct Batch {
     int n;
@@ -67,16 +67,17 @@ struct AppendParams {
 cudaError_t launch_append(const AppendParams& p, const Batch<AppendReq, kManyRequests>& batch, int num_sms, cudaStream_t stream);
 
 // ---- chunk_kernel.cu -----------------------------------------------------------------------------
-// Attention of the newest tokens of each request.  The query rows of a KV head are (token, query head of the group) pairs, the
+// Attention of the newest tokens of each request; a request may have several entries, one per set of query tiles.  The query rows of a KV head are (token, query head of the group) pairs, the
 // heads of a token side by side; a tile has the rows of kTile / group tokens.
 struct ChunkReq {
     int q_begin, n_new;          // its tokens on the packed axis
     int len;                     // cached rows, the new ones included
     int index;                   // of the request in the page table
     int unit_begin;              // units of the launch before its own
-    int n_sets;                  // two query tiles each, the last perhaps one
+    int set_begin, n_sets;       // sets of two query tiles (the request's last perhaps of one) that this entry has
     int step_begin;              // shares: steps of the launch before its own
     int head_steps;              // shares: steps of one of its KV heads
+    int pad;
     long long logits_begin;      // steps with weights: first logit of its [query head][row] block
 };
 // A unit of work: a set of query tiles of a KV head.
@@ -92,7 +93,7 @@ __host__ __device__
 #endif
 inline ChunkUnit chunk_unit(const ChunkReq& q, int set, int tile_tokens) {
     ChunkUnit u;
-    u.tok0 = set * 2 * tile_tokens;
+    u.tok0 = (q.set_begin + set) * 2 * tile_tokens;
     u.pair = u.tok0 + tile_tokens < q.n_new;
     const int before = q.len - q.n_new, first = u.tok0 + tile_tokens, second = first + tile_tokens;
     u.tiles0 = (before + (first < q.n_new ? first : q.n_new) + kTile - 1) / kTile;

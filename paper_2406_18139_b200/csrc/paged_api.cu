@@ -313,7 +313,7 @@ int chunk_attention(const void* q, const void* cache_k, const void* cache_v, flo
         c.len = lens[r];
         c.index = r;
         c.n_sets = ((c.n_new + tile_tokens - 1) / tile_tokens + 1) / 2;
-        c.unit_begin = c.step_begin = c.head_steps = 0;
+        c.unit_begin = c.set_begin = c.step_begin = c.head_steps = c.pad = 0;
         c.logits_begin = logits;
         if (c.len < c.n_new) return LOOKM_ERR_INVALID_ARG;
         logits += step ? (long long)c.len * paged->n_q_heads : 0;
@@ -329,7 +329,24 @@ int chunk_attention(const void* q, const void* cache_k, const void* cache_v, flo
     LOOKM_TRY(device_info(di));
     g_launches = 0;
     if (reqs.empty()) return LOOKM_OK;
-    std::stable_sort(reqs.begin(), reqs.end(), [](const ChunkReq& a, const ChunkReq& b) { return a.len > b.len; });
+    // Longest units first.  Of several requests with few sets every set is an entry of its own, so that the order is that of the sets
+    // (sixteen of 11 to 195 tokens over 2000 to 15000 rows, 32 heads on 8: 338 | 276 steps on the SM that has most).
+    long long sets = 0;
+    for (const ChunkReq& c : reqs) sets += c.n_sets;
+    if (reqs.size() > 1 && sets <= kManyRequests && sets > (long long)reqs.size()) {
+        std::vector<ChunkReq> each;
+        each.reserve(sets);
+        for (const ChunkReq& c : reqs)
+            for (int s = 0; s < c.n_sets; ++s) {
+                each.push_back(c);
+                each.back().set_begin = s;
+                each.back().n_sets = 1;
+            }
+        reqs.swap(each);
+    }
+    std::stable_sort(reqs.begin(), reqs.end(), [&](const ChunkReq& a, const ChunkReq& b) {
+        return chunk_unit(a, a.n_sets - 1, tile_tokens).steps > chunk_unit(b, b.n_sets - 1, tile_tokens).steps;
+    });
     CUtensorMap map_q, map_k, map_v;
     LOOKM_TRY(make_map_q(&map_q, q, tokens, paged, group, tile_tokens));
     LOOKM_TRY(make_map_pool(&map_k, cache_k, paged));
@@ -355,12 +372,13 @@ int chunk_attention(const void* q, const void* cache_k, const void* cache_v, flo
         Batch<ChunkReq, kManyRequests> b;
         b.n = (int)std::min<size_t>(kManyRequests, reqs.size() - base);
         b.pad = 0;
-        b.r[0] = reqs[base];
         long long total = 0;
         const bool shares = takes_shares(&reqs[base], b.n, tile_tokens, heads, rows, sms, &total);
         int ctas = sms;
         // Weights of short caches don't wait for a second launch.  (Of long ones half a CTA would take too long.)
-        p.mass_inside = step && b.r[0].len <= kMassInside;
+        int longest = 0;
+        for (int i = 0; i < b.n; ++i) longest = std::max(longest, reqs[base + i].len);
+        p.mass_inside = step && longest <= kMassInside;
         p.n_units = p.share = p.total_steps = 0;
         if (shares) {
             p.total_steps = (int)total;
