@@ -174,10 +174,12 @@ __device__ __forceinline__ bool warp_wait(unsigned long long* bar, uint32_t pari
 
 __device__ __forceinline__ bool odd_bf16(uint32_t x) { return (x & 0x7f80u) == 0x7f80u; }     // infinity or NaN
 
-// ---- warp 8 ---------------------------------------------------------------------------------------
+// ---- warp 8, and warp 11 where there are two loaders --------------------------------------------------
+// A copy of half the features of a page's rows takes some 65 clocks to issue: 1000 per tile of pages of 16 rows, more than memory needs for the
+// tile.  So two warps may take half of its pages each (p.loaders); warp 8 alone announces the bytes.
 template <int kRequests>
 __device__ __forceinline__ void load_tiles(const CUtensorMap& map_q, const CUtensorMap& map_k, const CUtensorMap& map_v,
-                                           const ChunkParams& p, const Batch<ChunkReq, kRequests>& batch, ChunkShared& sh) {
+                                           const ChunkParams& p, const Batch<ChunkReq, kRequests>& batch, ChunkShared& sh, int part) {
     const int lane = threadIdx.x & 31;
     volatile int* abort_flag = &sh.abort_flag;
     if (lane == 0) {
@@ -185,7 +187,7 @@ __device__ __forceinline__ void load_tiles(const CUtensorMap& map_q, const CUten
         ptx::prefetch_tensormap(&map_k);
         ptx::prefetch_tensormap(&map_v);
     }
-    const int box_rows = min(1 << p.pages.page_shift, kTile), boxes = kTile / box_rows;
+    const int box_rows = min(1 << p.pages.page_shift, kTile), boxes = kTile / box_rows / p.loaders, box = part * boxes + lane;
     const int q_bytes = p.tile_tokens * p.group * 256;
     uint32_t n = 0, nq = 0;                      // tiles and query tiles armed so far
     uint32_t dirty_phase = 0, last_dirty = 0;    // per stage: parity of its next use as a dirty one, whether its last use was one
@@ -194,7 +196,7 @@ __device__ __forceinline__ void load_tiles(const CUtensorMap& map_q, const CUten
     Item it;
     walk.start(p, batch);
     while (!stop && walk.next(p, batch, it)) {
-        for (int g = 0; g < (it.pair ? 2 : 1) && !stop; ++g, ++nq) {
+        for (int g = 0; part == 0 && g < (it.pair ? 2 : 1) && !stop; ++g, ++nq) {
             const int s = nq & 1;
             if (!warp_wait(&sh.q_empty[s], ((nq >> 1) & 1) ^ 1, abort_flag)) { stop = true; break; }
             if (lane == 0) {
@@ -205,28 +207,33 @@ __device__ __forceinline__ void load_tiles(const CUtensorMap& map_q, const CUten
                 ptx::tma_load_3d(dst + kHalfBytes, &map_q, 64, it.head * p.group, tok, bar);
             }
         }
-        // The page that this lane fetches for tile t (asked for a tile ahead); beyond the pool, which reads as zeros, if there is none.
+        // The table's entry for this lane's part of tile t, asked for a tile ahead and looked at when it is needed; where there is none, one
+        // beyond the pool, which reads as zeros.
         const auto page_for = [&](int t) {
-            const int row = (it.t0 + t) * kTile + lane * box_rows;
+            const int row = (it.t0 + t) * kTile + box * box_rows;
             if (t >= it.nt || lane >= boxes || row >= it.len) return p.pages.n_pages;
-            const int page = p.pages.page_of(it.index, row, p.status);
-            return page < 0 ? p.pages.n_pages : page;
+            return __ldg(p.pages.table + (long long)it.index * p.pages.table_stride + (row >> p.pages.page_shift));
         };
         const auto load = [&](const CUtensorMap& map, int t, int page, bool dirty) {
             if (stop) return;
             const int s = n % kRing;
             if (!warp_wait(&sh.empty[s], ((n / kRing) & 1) ^ 1, abort_flag)) { stop = true; return; }
             const uint32_t bar = ptx::smem_u32(dirty ? &sh.dirty[s] : &sh.full[s]);
-            if (lane == 0) {
+            if (part == 0 && lane == 0) {
                 ptx::mbar_arrive_expect_tx(bar, kTileBytes);
-                if (!dirty) ptx::mbar_arrive(bar);           // (the cleaning warps are two)
+                if (!dirty) ptx::mbar_arrive(bar);           // (a full tile takes two arrivals: the cleaning warps may be two)
             }
             last_dirty = (last_dirty & ~(1u << s)) | (dirty ? 1u << s : 0u);
             if (dirty) dirty_phase ^= 1u << s;
             __syncwarp();
             if (lane < boxes) {
-                const uint32_t dst = ptx::smem_u32(&sh.ring[s][0]) + lane * box_rows * 128;
-                const int in_page = ((it.t0 + t) * kTile + lane * box_rows) & ((1 << p.pages.page_shift) - 1);
+                if (page < 0 || page > p.pages.n_pages ||
+                    (page == p.pages.n_pages && (it.t0 + t) * kTile + box * box_rows < it.len)) {
+                    atomicMax(p.status, (int)LOOKM_ERR_DEVICE_BAD_INDEX);
+                    page = p.pages.n_pages;
+                }
+                const uint32_t dst = ptx::smem_u32(&sh.ring[s][0]) + box * box_rows * 128;
+                const int in_page = ((it.t0 + t) * kTile + box * box_rows) & ((1 << p.pages.page_shift) - 1);
                 ptx::tma_load_4d(dst, &map, 0, in_page, it.head, page, bar);
                 ptx::tma_load_4d(dst + kHalfBytes, &map, 64, in_page, it.head, page, bar);
             }
@@ -384,7 +391,9 @@ __device__ __forceinline__ void issue_mmas(const ChunkParams& p, const Batch<Chu
 // ---- warps 10 and 11 --------------------------------------------------------------------------------
 template <int kRequests>
 __device__ __forceinline__ void clean_values(const ChunkParams& p, const Batch<ChunkReq, kRequests>& batch, ChunkShared& sh) {
-    const int lane = threadIdx.x & 31, half = (threadIdx.x >> 5) - kCleanWarp;
+    const int lane = threadIdx.x & 31;
+    const bool alone = p.loaders == 2;          // (else the two warps have half of the features each)
+    const int half0 = alone ? 0 : (threadIdx.x >> 5) - kCleanWarp, half1 = alone ? 2 : half0 + 1;
     volatile int* abort_flag = &sh.abort_flag;
     uint32_t n = 0, n_items = 0, phase = 0;
     Walk walk;
@@ -400,24 +409,30 @@ __device__ __forceinline__ void clean_values(const ChunkParams& p, const Batch<C
             phase ^= 1u << s;
             const int row0 = (it.t0 + t) * kTile;
             const int end = min(max(it.len - row0, 0), kTile), all_see = min(max(it.min_seen - row0, 0), kTile);
-            uint4* v = reinterpret_cast<uint4*>(&sh.ring[s][half * kHalfBytes]);      // [128 rows][8]; within a row any order
-            for (int i = end * 8 + lane; i < kTile * 8; i += 32) v[i] = make_uint4(0, 0, 0, 0);
             bool odd = false;
-            for (int i = all_see * 8 + lane; i < end * 8; i += 32) {
-                uint4 x = v[i];
-                uint32_t* w = reinterpret_cast<uint32_t*>(&x);
-                bool here = false;
+            for (int half = half0; half < half1; ++half) {
+                uint4* v = reinterpret_cast<uint4*>(&sh.ring[s][half * kHalfBytes]);  // [128 rows][8]; within a row any order
+                for (int i = end * 8 + lane; i < kTile * 8; i += 32) v[i] = make_uint4(0, 0, 0, 0);
+#pragma unroll 4
+                for (int i = all_see * 8 + lane; i < end * 8; i += 32) {
+                    uint4 x = v[i];
+                    uint32_t* w = reinterpret_cast<uint32_t*>(&x);
+                    bool here = false;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if (odd_bf16(w[j])) { w[j] &= 0xffff0000u; here = true; }
-                    if (odd_bf16(w[j] >> 16)) { w[j] &= 0xffffu; here = true; }
+                    for (int j = 0; j < 4; ++j) {
+                        if (odd_bf16(w[j])) { w[j] &= 0xffff0000u; here = true; }
+                        if (odd_bf16(w[j] >> 16)) { w[j] &= 0xffffu; here = true; }
+                    }
+                    if (here) { v[i] = x; odd = true; }
                 }
-                if (here) { v[i] = x; odd = true; }
             }
             if (odd) sh.odd_values[n_items % kFlags] = (int)n_items + 1;
             ptx::fence_proxy_async_shared();
             __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&sh.full[s]));
+            if (lane == 0) {
+                ptx::mbar_arrive(ptx::smem_u32(&sh.full[s]));
+                if (alone) ptx::mbar_arrive(ptx::smem_u32(&sh.full[s]));
+            }
         }
         n += 2 * it.nt;
         ++n_items;
@@ -742,9 +757,11 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
     } else {
         ptx::fewer_registers<kOtherRegs>();
         if (warp == kLoadWarp) {
-            load_tiles(map_q, map_k, map_v, p, batch, sh);
+            load_tiles(map_q, map_k, map_v, p, batch, sh, 0);
         } else if (warp == kMmaWarp) {
             issue_mmas(p, batch, sh, tmem);
+        } else if (warp == kCleanWarp + 1 && p.loaders == 2) {
+            load_tiles(map_q, map_k, map_v, p, batch, sh, 1);
         } else {
             clean_values(p, batch, sh);
         }

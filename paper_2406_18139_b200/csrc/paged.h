@@ -117,6 +117,7 @@ struct ChunkParams {
     int n_tokens;                // on the packed axis (= the row stride of lse)
     int share;                   // > 0: the CTAs take so many steps each of all units' ...
     int total_steps;             // ... which are so many; units that are cut leave partial rows
+    int loaders;                 // warps that load the cached rows: 1 or 2
     int slot_rows;               // partial rows of a piece: two pieces per CTA, its first and its last
     float scale_log2;            // softmax scale * log2(e)
     const void* cache_v;

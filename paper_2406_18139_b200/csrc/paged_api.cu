@@ -355,6 +355,10 @@ int chunk_attention(const void* q, const void* cache_k, const void* cache_v, flo
     p.pages = pages_of(paged, table);
     p.group = group;
     p.tile_tokens = tile_tokens;
+    // Two warps load pages of 16 rows where every unit has one query tile and so memory is the bound (sixteen single tokens over 400 to 8192
+    // rows, 32 heads on 8, us, one | two: 59.5 | 56.5); one of them is then missing where values are looked over (a prompt of 4096
+    // x 32: 135 | 151).  Pages of 32 rows: 54.3 | 56.4.
+    p.loaders = paged->page_rows == 16 && most_new <= tile_tokens ? 2 : 1;
     p.slot_rows = rows;
     p.n_tokens = (int)tokens;
     p.scale_log2 = (paged->softmax_scale > 0.f ? paged->softmax_scale : 1.0f / std::sqrt((float)kHeadDim)) * 1.4426950408889634f;
