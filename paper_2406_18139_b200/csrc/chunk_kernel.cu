@@ -4,19 +4,32 @@
 //
 // chunk_kernel: persistent, one CTA per SM.  Two streams of work run side by side, each with a 128 x 128 fp32 block of logits
 // and one of outputs in tensor memory (all 512 columns) and a warpgroup that turns logits into probabilities; while one
-// warpgroup works, the tensor core multiplies for the other.  An item is one KV head of one request with
+// warpgroup works, the tensor core multiplies for the other.  A unit of work is one KV head of one request with
 //   two query tiles (128 rows each: tokens x query heads of the group): both streams meet every tile of 128 cached rows, or
-//   one query tile: the streams take the cached rows' tiles alternately and are added up at the end,
-// over all rows that these tokens see or over a range of them (few items: the ranges are added up by chunk_finish_kernel).
+//   one query tile: the streams take the cached rows' tiles alternately and are added up at the end.
+// CTAs take whole units or, where these leave SMs idle, equal shares of all units' tiles (the pieces of units that are cut are
+// added up by a second launch).
 //   warps 0-3, 4-7  softmax of stream 0 and 1: a thread has a row of logits.  Probabilities become bf16 (the type of V, which
-//                   the tensor core wants on both sides: an error of at most 2^-8 each that averages out over the row's sum, no larger than the output's own
-//                   rounding) and lie where the logits lay, as the A operand of P V.  Sums stay fp32.  The reference that is subtracted follows the
-//                   maximum only when that has grown by 2^8, so outputs are seldom rescaled
+//                   the tensor core wants on both sides: an error of at most 2^-8 each that averages out over the row's sum, no
+//                   larger than the output's own rounding) and lie where the logits lay, as the A operand of P V.  Sums stay
+//                   fp32.  The reference that is subtracted follows the maximum only when that has grown by 2^8, so outputs are
+//                   seldom rescaled
 //   warp 8          query tiles and cached rows by TMA, page by page, into one ring of tiles for K and V alternately
 //   warp 9          issues the MMAs: S = Q K^T, O += P V.  They run in the order they are issued in, so the next S may
 //                   overwrite the P that the product before it reads
-//   warps 10-11     V rows that not every row of the item sees: what lies behind the cache's end becomes zero, and so do infinities and
-//                   NaN (0 times which would be NaN in rows that don't see them); rows that do see them get them in the epilogue
+//   warps 10-11     V rows that not every row of the unit sees: what lies behind the cache's end becomes zero, and so do
+//                   infinities and NaN (0 times which would be NaN in rows that don't see them); rows that do see them get
+//                   them in the epilogue
+//
+// What bounds it.  Many query rows: the hand-overs from softmax to issuing warp to tensor core and back, some 1200 of 3600 clocks per
+// two tiles; then the softmax (1900) and the products (2048), which overlap.  8192 tokens x 32 heads 468 us = 1.17 PFLOP/s, in a long
+// row of calls 550 us at the board's power limit (tensor pipe half busy, special-function unit half).  Without exponentials 460,
+// without any softmax arithmetic 417, with an eighth of P V 413, of Q K^T 397, of both 375.
+// Slower: one issuing warp per stream (561: their products take turns and both streams wait longer), sixteen softmax warps with
+// half a row each (582: 104 registers do not do), exponentials partly on the FMA pipe (+3 to 7 %), the reference from the tiles
+// before so that exponentials need not wait for the maximum (500), polling instead of suspended waits (490).
+// Few query rows: memory.  Sixteen single tokens over 400 to 8192 rows, 32 heads on 8, 57 us = 4.9 TB/s; with weights, over 400 to
+// 16384, 109 us.
 #include <algorithm>
 
 #include <cuda_bf16.h>
