@@ -328,7 +328,7 @@ int lookm_step_attention(const void* q, const void* cache_k, const void* cache_v
 /* Eviction by accumulated attention weight, per request and KV head: with B = min(budget, len) the last
  * min(window, B) rows stay and, of the others, the heaviest until there are B (the lower row among equals; NaN counts
  * as lightest); they become rows 0 .. B - 1 in their order.
- *   out_k, out_v, out_mass, out_page_table   where the rows go; same layout.  Either the cache itself (in place: the same
+ *   out_k, out_v, out_mass, out_page_table   where the rows go; same layout and table_stride.  Either the cache itself (in place: the same
  *               pools, and a table that has the same page at the same place or one that `page_table` does not
  *               have at all), or pools and pages that overlap none of the input's.  Requests must not share pages that
  *               are written.  Rows from B on are left as they are.

@@ -449,7 +449,8 @@ def lookm_evict(cache_k, cache_v, mass, page_table, cache_lens, budgets, windows
     n = len(cache_lens)
     if len(budgets) != n or len(windows) != n or not _here(n, page_table, (cache_k, cache_v, mass, page_table, out_k, out_v, out_mass,
                                                                            out_page_table, kept_idx, workspace)) \
-            or out_page_table.dtype is not page_table.dtype or out_page_table.shape[0] < n:
+            or out_page_table.dtype is not page_table.dtype or out_page_table.shape[0] < n \
+            or (n > 1 and out_page_table.stride(0) != page_table.stride(0)):
         return ERR_INVALID_ARG
     return lib().lookm_evict(_ptr(cache_k), _ptr(cache_v), _ptr(mass), _ptr(page_table), _ints(cache_lens), _ints(budgets),
                              _ints(windows), n, C.byref(paged), _ptr(out_k), _ptr(out_v), _ptr(out_mass),

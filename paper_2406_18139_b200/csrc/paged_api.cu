@@ -15,6 +15,10 @@ constexpr int kMaxLen = 1 << 25;         // rows of a cache, tokens of a call
 
 bool aligned(const void* p, unsigned bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 
+float scale_log2(const lookm_paged_layout* l) {
+    return (l->softmax_scale > 0.f ? l->softmax_scale : 1.0f / std::sqrt((float)kHeadDim)) * 1.4426950408889634f;
+}
+
 int check_paged(const lookm_paged_layout* l) {
     if (!l) return LOOKM_ERR_INVALID_ARG;
     if (l->head_dim != kHeadDim) return LOOKM_ERR_UNSUPPORTED;
@@ -26,7 +30,7 @@ int check_paged(const lookm_paged_layout* l) {
         if (s < kHeadDim || s % 8) return LOOKM_ERR_INVALID_ARG;
         if (s >= (1ll << 38)) return LOOKM_ERR_UNSUPPORTED;          // (tensor maps keep 40 bits of bytes)
     }
-    if (!(l->softmax_scale >= 0.f) || !std::isfinite(l->softmax_scale)) return LOOKM_ERR_INVALID_ARG;
+    if (!(l->softmax_scale >= 0.f) || !std::isfinite(scale_log2(l))) return LOOKM_ERR_INVALID_ARG;
     return LOOKM_OK;
 }
 
@@ -361,7 +365,7 @@ int chunk_attention(const void* q, const void* cache_k, const void* cache_v, flo
     p.loaders = paged->page_rows == 16 && most_new <= tile_tokens ? 2 : 1;
     p.slot_rows = rows;
     p.n_tokens = (int)tokens;
-    p.scale_log2 = (paged->softmax_scale > 0.f ? paged->softmax_scale : 1.0f / std::sqrt((float)kHeadDim)) * 1.4426950408889634f;
+    p.scale_log2 = scale_log2(paged);
     p.cache_v = cache_v;
     p.out = out;
     p.lse = lse ? lse : step ? at<float>(ws, space.lse) : nullptr;

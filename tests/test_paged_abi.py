@@ -48,7 +48,7 @@ CALLS = [append, chunk, step, evict]
 
 @pytest.mark.parametrize("call", CALLS)
 def test_layouts(call):
-    bad = dict(hq=0), dict(hkv=0), dict(hq=7), dict(pages=0), dict(stride=0), dict(scale=-1.0), dict(scale=float("nan")), \
+    bad = dict(hq=0), dict(hkv=0), dict(hq=7), dict(pages=0), dict(stride=0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=3e38), \
         dict(page_stride=0), dict(row_stride=64), dict(head_stride=132), dict(page_stride=-256)
     for kw in bad:
         assert call(paged(**kw)) == B.ERR_INVALID_ARG, kw
@@ -143,4 +143,6 @@ def test_binding_refuses_what_the_library_cannot_see():
     assert ok(k=cpu) == ok(cu=[0, 1, 1]) == ok(table=table.long()) == ok(table=table[:0]) == B.ERR_INVALID_ARG
     assert B.lookm_step_attention(q, gpu, gpu, mass.cpu(), table, [5], lay, out, None, ws) == B.ERR_INVALID_ARG
     assert B.lookm_evict(gpu, gpu, mass, table, [5], [3, 3], [1], lay, gpu, gpu, mass, table, None, ws) == B.ERR_INVALID_ARG
+    two, wide = torch.zeros(2, 4, dtype=torch.int32, device="cuda"), torch.zeros(2, 5, dtype=torch.int32, device="cuda")
+    assert B.lookm_evict(gpu, gpu, mass, two, [5, 5], [3, 3], [1, 1], lay, gpu, gpu, mass, wide, None, ws) == B.ERR_INVALID_ARG
 
