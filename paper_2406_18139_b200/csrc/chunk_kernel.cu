@@ -462,12 +462,13 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 // pages, logits of two heads and masses asked for together.
 __device__ __forceinline__ void add_weights(const ChunkParams& p, int index, int head, int len, const float* logits, const float* lse2, int t,
                                             int end, int stride) {
+    const long long row = logits_stride(len);
     for (; t < end; t += 4 * stride) {
         int page[4];
         float w[4] = {0.f, 0.f, 0.f, 0.f}, m[4], x[2][4];
         const auto ask = [&](int g, float (&y)[4]) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) y[j] = t + j * stride < end ? logits[(long long)g * len + t + j * stride] : 0.f;
+            for (int j = 0; j < 4; ++j) y[j] = t + j * stride < end ? logits[g * row + t + j * stride] : 0.f;
         };
         const auto add = [&](int g, const float (&y)[4]) {
 #pragma unroll
@@ -529,7 +530,7 @@ __device__ __forceinline__ void softmax_rows(const ChunkParams& p, const Batch<C
         const int seen = live ? it.len - it.n_new + tok + 1 : 0x7fffffff;
         const int nt = g ? it.nt1 : it.nt0, t_first = it.t0 + (it.pair ? 0 : g), t_step = it.pair ? 1 : 2;
         float* to_logits = nullptr;
-        if constexpr (kStep) to_logits = p.logits + it.logits_begin + (long long)q_head * it.len;
+        if constexpr (kStep) to_logits = p.logits + it.logits_begin + (long long)q_head * logits_stride(it.len);
         float m = -INFINITY, l = 0.f;            // reference, sum
         for (int j = 0; j < nt; ++j, ++n) {
             const int t = t_first + j * t_step;
@@ -543,10 +544,13 @@ __device__ __forceinline__ void softmax_rows(const ChunkParams& p, const Batch<C
                 const bool masked = __any_sync(0xffffffffu, cols < kTile);
                 ptx::tmem_ld_wait();
                 if constexpr (kStep) {
-                    if (live) {                  // (a step's rows see all that is cached)
+                    if (live) {                  // (a step's rows see all that is cached; a row of logits has room for whole fours)
+                        uint4* to_logits4 = reinterpret_cast<uint4*>(to_logits + t * kTile);
 #pragma unroll
-                        for (int i = 0; i < kTile; ++i)
-                            if (i < cols) to_logits[t * kTile + i] = __uint_as_float(s[i >> 5][i & 31]);
+                        for (int i = 0; i < kTile / 4; ++i)
+                            if (4 * i < cols)
+                                to_logits4[i] = make_uint4(s[i >> 3][4 * i & 31], s[i >> 3][(4 * i & 31) + 1], s[i >> 3][(4 * i & 31) + 2],
+                                                           s[i >> 3][(4 * i & 31) + 3]);
                     }
                     __syncwarp();
                 }
@@ -711,7 +715,7 @@ __device__ __forceinline__ void softmax_rows(const ChunkParams& p, const Batch<C
                 if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&sh.lse_full));
                 if (!warp_wait(&sh.lse_full, n_masses & 1, abort_flag)) return;
                 ++n_masses;
-                add_weights(p, it.index, it.head, it.len, p.logits + it.logits_begin + (long long)it.head * p.group * it.len, sh.lse2, row, it.len,
+                add_weights(p, it.index, it.head, it.len, p.logits + it.logits_begin + (long long)it.head * p.group * logits_stride(it.len), sh.lse2, row, it.len,
                             kTile);
             }
         }
@@ -919,7 +923,7 @@ step_finish_kernel(const __grid_constant__ ChunkParams p, const __grid_constant_
     }
     __syncthreads();
     const int t0 = blockIdx.y * kMassRows;
-    add_weights(p, q.index, head, q.len, p.logits + q.logits_begin + (long long)head * p.group * q.len, lse2, t0 + threadIdx.x,
+    add_weights(p, q.index, head, q.len, p.logits + q.logits_begin + (long long)head * p.group * logits_stride(q.len), lse2, t0 + threadIdx.x,
                 min(q.len, t0 + kMassRows), kFinishThreads);
 }
 

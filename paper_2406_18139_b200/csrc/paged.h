@@ -80,6 +80,11 @@ struct ChunkReq {
     int pad;
     long long logits_begin;      // steps with weights: first logit of its [query head][row] block
 };
+// Floats between two query heads' logits of a step: whole fours, for wide stores.
+#ifdef __CUDACC__
+__host__ __device__
+#endif
+inline long long logits_stride(int len) { return (len + 3) & ~3; }
 // A unit of work: a set of query tiles of a KV head.
 struct ChunkUnit {
     int tok0;                    // first token

@@ -320,7 +320,7 @@ int chunk_attention(const void* q, const void* cache_k, const void* cache_v, flo
         c.unit_begin = c.set_begin = c.step_begin = c.head_steps = c.pad = 0;
         c.logits_begin = logits;
         if (c.len < c.n_new) return LOOKM_ERR_INVALID_ARG;
-        logits += step ? (long long)c.len * paged->n_q_heads : 0;
+        logits += step ? logits_stride(c.len) * paged->n_q_heads : 0;
         if (c.n_new) reqs.push_back(c);
         most_new = std::max<long long>(most_new, c.n_new);
         units += (long long)c.n_sets * paged->n_kv_heads;
@@ -423,15 +423,16 @@ extern "C" {
 size_t lookm_paged_workspace_size(const lookm_paged_layout* paged, int n_requests, const int* new_lens_host,
                                   const int* cache_lens_host) {
     if (check_paged(paged) != LOOKM_OK || check_requests(paged, n_requests, cache_lens_host) != LOOKM_OK) return 0;
-    size_t rows = 0, tokens = 0;
+    size_t rows = 0, tokens = 0, logits = 0;
     for (int r = 0; r < n_requests; ++r) {
         if (new_lens_host && new_lens_host[r] < 0) return 0;
         rows += cache_lens_host[r];
+        logits += logits_stride(cache_lens_host[r]) * paged->n_q_heads;
         tokens += new_lens_host ? new_lens_host[r] : 1;
     }
     long long most_new = 1;
     for (int r = 0; r < n_requests; ++r) most_new = std::max<long long>(most_new, new_lens_host ? new_lens_host[r] : 1);
-    const size_t attention = chunk_space(slot_rows(paged, most_new), rows * paged->n_q_heads,
+    const size_t attention = chunk_space(slot_rows(paged, most_new), logits,
                                          std::max(tokens, (size_t)n_requests) * paged->n_q_heads).total;
     return std::max(align_up(kStatusBytes + 4 * rows * paged->n_kv_heads, 256), attention);
 }
