@@ -880,7 +880,7 @@ __device__ __forceinline__ void add_pieces(const ChunkParams& p, const ChunkReq&
 }
 // ... all rows of the unit, `stride` half-warps from number `first` on
 __device__ __forceinline__ void add_pieces_of_rows(const ChunkParams& p, const ChunkReq& q, const Cuts& cuts, int head, int first, int stride) {
-    const int rows = min(q.n_new - cuts.u.tok0, 2 * p.tile_tokens) * p.group;
+    const int rows = min(q.n_new - cuts.u.tok0, q.set_tiles * p.tile_tokens) * p.group;
     const int half = (threadIdx.x >> 4) & 1;
     for (int row = first - half; row < rows; row += stride) add_pieces(p, q, cuts, head, min(row + half, rows - 1));
 }

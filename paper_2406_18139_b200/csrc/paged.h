@@ -74,10 +74,10 @@ struct ChunkReq {
     int len;                     // cached rows, the new ones included
     int index;                   // of the request in the page table
     int unit_begin;              // units of the launch before its own
-    int set_begin, n_sets;       // sets of two query tiles (the request's last perhaps of one) that this entry has
+    int set_begin, n_sets;       // sets of query tiles that this entry has
     int step_begin;              // shares: steps of the launch before its own
     int head_steps;              // shares: steps of one of its KV heads
-    int pad;
+    int set_tiles;               // query tiles of a set: 2 (the request's last set perhaps 1), or 1
     long long logits_begin;      // steps with weights: first logit of its [query head][row] block
 };
 // Floats between two query heads' logits of a step: whole fours, for wide stores.
@@ -98,8 +98,8 @@ __host__ __device__
 #endif
 inline ChunkUnit chunk_unit(const ChunkReq& q, int set, int tile_tokens) {
     ChunkUnit u;
-    u.tok0 = (q.set_begin + set) * 2 * tile_tokens;
-    u.pair = u.tok0 + tile_tokens < q.n_new;
+    u.tok0 = (q.set_begin + set) * q.set_tiles * tile_tokens;
+    u.pair = q.set_tiles == 2 && u.tok0 + tile_tokens < q.n_new;
     const int before = q.len - q.n_new, first = u.tok0 + tile_tokens, second = first + tile_tokens;
     u.tiles0 = (before + (first < q.n_new ? first : q.n_new) + kTile - 1) / kTile;
     u.tiles = u.pair ? (before + (second < q.n_new ? second : q.n_new) + kTile - 1) / kTile : u.tiles0;

@@ -241,29 +241,64 @@ int slot_rows(const lookm_paged_layout* l, long long most_new) {
     return (int)std::min<long long>(2ll * (kTile / group) * group, std::max<long long>(most_new, 1) * group);
 }
 
+// The steps of all units, and of the CTA that has most in the kernel's deal of whole units (0: so many units that they even out).
+struct Deal { long long steps, most; };
+Deal deal(const ChunkReq* reqs, int n, int tile_tokens, int heads, int sms) {
+    long long units = 0;
+    Deal d = {0, 0};
+    for (int r = 0; r < n; ++r) units += (long long)reqs[r].n_sets * heads;
+    if (units >= 4ll * sms) return d;
+    long long load[kMaxCtas] = {};
+    int i = 0, step = 1;
+    for (int r = 0; r < n; ++r)
+        for (int s = reqs[r].n_sets - 1; s >= 0; --s) {
+            const int k = chunk_unit(reqs[r], s, tile_tokens).steps;
+            d.steps += (long long)k * heads;
+            for (int h = 0; h < heads; ++h) {
+                d.most = std::max(d.most, load[i] += k);
+                i += step;
+                if (i == sms || i < 0) { i -= step; step = -step; }
+            }
+        }
+    return d;
+}
+
 // Whether the CTAs of a launch take equal shares of all units' steps instead of whole units: where the SM with the most whole units
 // would be busy for longer than a share, a second launch and what the pieces' partial rows cost.  A step takes about
 // 1 us.  us, whole | shares: one prompt of 4096 tokens x 32 heads 131 | 163, 512 tokens over 32256, 32 heads on 8, 433 | 256, 8 x 256 over
 // 9000, 8 heads, 132 | 100, 16 x 128 over 9000, 32 on 8, 284 | 310, 100 over 5000 x 40 49 | 34, one over 2000 x 32 21.6 | 18.3, four
 // of one over 1000 to 3000 x 32 35.1 | 36.3.
+long long in_shares(const Deal& d, int rows, int sms) { return (d.steps + sms - 1) / sms + 8 + rows / 8; }
 bool takes_shares(const ChunkReq* reqs, int n, int tile_tokens, int heads, int rows, int sms, long long* total) {
-    long long units = 0, steps = 0;
-    for (int r = 0; r < n; ++r) units += (long long)reqs[r].n_sets * heads;
-    if (units >= 4ll * sms) return false;
-    long long load[kMaxCtas] = {}, most = 0;         // the kernel's own deal of whole units
-    int i = 0, step = 1;
-    for (int r = 0; r < n; ++r)
-        for (int s = reqs[r].n_sets - 1; s >= 0; --s) {
-            const int k = chunk_unit(reqs[r], s, tile_tokens).steps;
-            steps += (long long)k * heads;
-            for (int h = 0; h < heads; ++h) {
-                most = std::max(most, load[i] += k);
-                i += step;
-                if (i == sms || i < 0) { i -= step; step = -step; }
-            }
+    const Deal d = deal(reqs, n, tile_tokens, heads, sms);
+    *total = d.steps;
+    return d.most > 0 && d.steps < (1ll << 30) && d.most > in_shares(d, rows, sms);
+}
+
+// The entries of a call's requests in the order in which their units are dealt: longest units first.  Of several requests with few
+// sets every set is an entry of its own, so that the order is that of the sets (sixteen of 11 to 195 tokens over 2000 to 15000 rows, 32 heads
+// on 8: 338 | 276 steps on the SM that has most).
+std::vector<ChunkReq> chunk_entries(const std::vector<ChunkReq>& reqs, int tile_tokens, int set_tiles) {
+    std::vector<ChunkReq> all;
+    long long sets = 0;
+    for (const ChunkReq& q : reqs) sets += ((q.n_new + tile_tokens - 1) / tile_tokens + set_tiles - 1) / set_tiles;
+    const bool each = reqs.size() > 1 && sets <= kManyRequests;
+    all.reserve(each ? sets : reqs.size());
+    for (ChunkReq q : reqs) {
+        q.set_tiles = set_tiles;
+        q.n_sets = ((q.n_new + tile_tokens - 1) / tile_tokens + set_tiles - 1) / set_tiles;
+        if (!each || q.n_sets == 1) {
+            all.push_back(q);
+            continue;
         }
-    *total = steps;
-    return steps < (1ll << 30) && most > (steps + sms - 1) / sms + 8 + rows / 8;
+        const int n = q.n_sets;
+        q.n_sets = 1;
+        for (q.set_begin = 0; q.set_begin < n; ++q.set_begin) all.push_back(q);
+    }
+    std::stable_sort(all.begin(), all.end(), [&](const ChunkReq& a, const ChunkReq& b) {
+        return chunk_unit(a, a.n_sets - 1, tile_tokens).steps > chunk_unit(b, b.n_sets - 1, tile_tokens).steps;
+    });
+    return all;
 }
 
 // bf16 [tokens, heads, 128]: boxes of the rows of a query tile
@@ -316,8 +351,9 @@ int chunk_attention(const void* q, const void* cache_k, const void* cache_v, flo
         c.n_new = step ? 1 : cu[r + 1] - cu[r];
         c.len = lens[r];
         c.index = r;
-        c.n_sets = ((c.n_new + tile_tokens - 1) / tile_tokens + 1) / 2;
-        c.unit_begin = c.set_begin = c.step_begin = c.head_steps = c.pad = 0;
+        c.n_sets = (c.n_new + tile_tokens - 1) / tile_tokens;
+        c.unit_begin = c.set_begin = c.step_begin = c.head_steps = 0;
+        c.set_tiles = 1;
         c.logits_begin = logits;
         if (c.len < c.n_new) return LOOKM_ERR_INVALID_ARG;
         logits += step ? logits_stride(c.len) * paged->n_q_heads : 0;
@@ -333,24 +369,25 @@ int chunk_attention(const void* q, const void* cache_k, const void* cache_v, flo
     LOOKM_TRY(device_info(di));
     g_launches = 0;
     if (reqs.empty()) return LOOKM_OK;
-    // Longest units first.  Of several requests with few sets every set is an entry of its own, so that the order is that of the sets
-    // (sixteen of 11 to 195 tokens over 2000 to 15000 rows, 32 heads on 8: 338 | 276 steps on the SM that has most).
-    long long sets = 0;
-    for (const ChunkReq& c : reqs) sets += c.n_sets;
-    if (reqs.size() > 1 && sets <= kManyRequests && sets > (long long)reqs.size()) {
-        std::vector<ChunkReq> each;
-        each.reserve(sets);
-        for (const ChunkReq& c : reqs)
-            for (int s = 0; s < c.n_sets; ++s) {
-                each.push_back(c);
-                each.back().set_begin = s;
-                each.back().n_sets = 1;
+    // Sets of one query tile where sets of two would leave SMs idle.  A step of a single tile takes 1.3 times a pair's, with pages of 16
+    // rows, whose loading is the bound, 1.65 times.  us, pairs | singles: one prompt of 2048 tokens x 8 heads 35 | 25, of 4096 x 8 65 | 42, of 2048 x 32
+    // 45 | 55, four of 128 tokens over 3000, 32 heads on 8, 53 | 34, eight of 256 over 9000, 8 heads, 104 | 93; two of 60 over 4000, 32 on 8,
+    // pages of 16, 37 | 56.
+    const int sms = std::min(di.sms, kMaxCtas), heads = paged->n_kv_heads;
+    std::vector<ChunkReq> entries = chunk_entries(reqs, tile_tokens, 2);
+    if (most_new > tile_tokens && entries.size() <= (size_t)kManyRequests) {
+        const Deal two = deal(entries.data(), (int)entries.size(), tile_tokens, heads, sms);
+        if (two.most > 0) {
+            std::vector<ChunkReq> singles = chunk_entries(reqs, tile_tokens, 1);
+            if (singles.size() <= (size_t)kManyRequests) {
+                const Deal one = deal(singles.data(), (int)singles.size(), tile_tokens, heads, sms);
+                const long long in_ones = std::min(one.most, in_shares(one, std::min(rows, kTile), sms)),
+                                in_twos = std::min(two.most, in_shares(two, rows, sms));
+                if (one.most > 0 && (paged->page_rows == 16 ? 33 : 26) * in_ones < 20 * in_twos) entries.swap(singles);
             }
-        reqs.swap(each);
+        }
     }
-    std::stable_sort(reqs.begin(), reqs.end(), [&](const ChunkReq& a, const ChunkReq& b) {
-        return chunk_unit(a, a.n_sets - 1, tile_tokens).steps > chunk_unit(b, b.n_sets - 1, tile_tokens).steps;
-    });
+    reqs.swap(entries);
     CUtensorMap map_q, map_k, map_v;
     LOOKM_TRY(make_map_q(&map_q, q, tokens, paged, group, tile_tokens));
     LOOKM_TRY(make_map_pool(&map_k, cache_k, paged));
@@ -375,13 +412,12 @@ int chunk_attention(const void* q, const void* cache_k, const void* cache_v, flo
     p.mass = mass;
     p.status = at<int>(ws, 0);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const int sms = std::min(di.sms, kMaxCtas), heads = paged->n_kv_heads;
     for (size_t base = 0; base < reqs.size(); base += kManyRequests) {
         Batch<ChunkReq, kManyRequests> b;
         b.n = (int)std::min<size_t>(kManyRequests, reqs.size() - base);
         b.pad = 0;
         long long total = 0;
-        const bool shares = takes_shares(&reqs[base], b.n, tile_tokens, heads, rows, sms, &total);
+        const bool shares = takes_shares(&reqs[base], b.n, tile_tokens, heads, reqs[base].set_tiles == 1 ? std::min(rows, kTile) : rows, sms, &total);
         int ctas = sms;
         // Weights of short caches don't wait for a second launch.  (Of long ones half a CTA would take too long.)
         int longest = 0;
