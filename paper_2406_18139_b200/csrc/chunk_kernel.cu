@@ -36,7 +36,7 @@
 #include <math.h>
 
 #include "paged.h"
-#include "ptx.cuh"
+#include "ptx_paged.cuh"
 
 namespace lookm {
 namespace {
@@ -463,6 +463,7 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 __device__ __forceinline__ void add_weights(const ChunkParams& p, int index, int head, int len, const float* logits, const float* lse2, int t,
                                             int end, int stride) {
     const long long row = logits_stride(len);
+    const int* table = p.pages.table + (long long)index * p.pages.table_stride;
     for (; t < end; t += 4 * stride) {
         int page[4];
         float w[4] = {0.f, 0.f, 0.f, 0.f}, m[4], x[2][4];
@@ -476,7 +477,7 @@ __device__ __forceinline__ void add_weights(const ChunkParams& p, int index, int
         };
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-            page[j] = t + j * stride < end ? __ldg(p.pages.table + (long long)index * p.pages.table_stride + ((t + j * stride) >> p.pages.page_shift)) : 0;
+            page[j] = t + j * stride < end ? __ldg(table + ((t + j * stride) >> p.pages.page_shift)) : 0;
         ask(0, x[0]);
         if (p.group > 1) ask(1, x[1]);
 #pragma unroll
@@ -715,8 +716,8 @@ __device__ __forceinline__ void softmax_rows(const ChunkParams& p, const Batch<C
                 if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&sh.lse_full));
                 if (!warp_wait(&sh.lse_full, n_masses & 1, abort_flag)) return;
                 ++n_masses;
-                add_weights(p, it.index, it.head, it.len, p.logits + it.logits_begin + (long long)it.head * p.group * logits_stride(it.len), sh.lse2, row, it.len,
-                            kTile);
+                add_weights(p, it.index, it.head, it.len, p.logits + it.logits_begin + (long long)it.head * p.group * logits_stride(it.len),
+                            sh.lse2, row, it.len, kTile);
             }
         }
         ++n_items;

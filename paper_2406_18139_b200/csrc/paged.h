@@ -67,8 +67,9 @@ struct AppendParams {
 cudaError_t launch_append(const AppendParams& p, const Batch<AppendReq, kManyRequests>& batch, int num_sms, cudaStream_t stream);
 
 // ---- chunk_kernel.cu -----------------------------------------------------------------------------
-// Attention of the newest tokens of each request; a request may have several entries, one per set of query tiles.  The query rows of a KV head are (token, query head of the group) pairs, the
-// heads of a token side by side; a tile has the rows of kTile / group tokens.
+// Attention of the newest tokens of each request; a request may have several entries, one per set of query tiles.  The query rows
+// of a KV head are (token, query head of the group) pairs, the heads of a token side by side; a tile has the rows of kTile / group
+// tokens.
 struct ChunkReq {
     int q_begin, n_new;          // its tokens on the packed axis
     int len;                     // cached rows, the new ones included
