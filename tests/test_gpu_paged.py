@@ -161,7 +161,8 @@ def run_evict(B, lens, budgets, windows, hkv, page, in_place, mass=None, heads_f
     ([1], [1], [0], 1, 16), ([2], [1], [0], 1, 16), ([2], [1], [1], 1, 16), ([17], [16], [4], 3, 16), ([100], [100], [10], 2, 32),
     ([100], [999], [10], 2, 32), ([700], [140], [16], 4, 16), ([700], [140], [140], 4, 16), ([700], [140], [500], 4, 64),
     ([33, 0, 500], [20, 5, 499], [3, 1, 8], 5, 16), ([8192], [1638], [32], 8, 16), ([2048, 2049], [2047, 1], [0, 0], 2, 128),
-    ([5000, 1200, 37], [4000, 960, 29], [32, 32, 32], 32, 64), ([33000], [30000], [64], 2, 64), ([40000], [9000], [7], 1, 256),
+    ([5000, 1200, 37], [4000, 960, 29], [32, 32, 32], 32, 64), ([33000], [30000], [64], 2, 64), ([40000], [9000], [7], 1, 256), ([300000], [100000], [33], 1, 256),
+    ([36000, 50], [1000, 49], [9, 9], 80, 64),
     ([40] * 131, [20] * 131, [2] * 131, 2, 16)])
 def test_evict_keeps_the_heaviest_rows(B, in_place, lens, budgets, windows, hkv, page):
     run_evict(B, lens, budgets, windows, hkv, page, in_place, seed=sum(lens), heads_first=hkv % 2 == 0)
