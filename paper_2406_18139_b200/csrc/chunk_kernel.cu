@@ -619,6 +619,7 @@ __device__ __forceinline__ void softmax_rows(const ChunkParams& p, const Batch<C
             if (!warp_wait(&sh.merge_free, (n_merges & 1) ^ 1, abort_flag)) return;
             sh.merge_m[row] = m;
             sh.merge_l[row] = l;
+            ptx::tc_fence_before_sync();         // (stream 0 reads the output block that this one has waited for, and has rescaled)
             __syncwarp();
             if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&sh.merge_full));
             ++n_merges;
@@ -628,6 +629,7 @@ __device__ __forceinline__ void softmax_rows(const ChunkParams& p, const Batch<C
         float scale0 = 1.f, scale1 = 0.f, total = l, top = m;
         if (!it.pair) {
             if (!warp_wait(&sh.merge_full, n_merges & 1, abort_flag)) return;
+            ptx::tc_fence_after_sync();          // (of stream 1's outputs only stream 1's warps know that they are there)
             ++n_merges;
             const float m1 = sh.merge_m[row], l1 = sh.merge_l[row];
             __syncwarp();
