@@ -45,7 +45,9 @@ constexpr int kSoftmaxWarps = 8, kLoadWarp = 8, kMmaWarp = 9, kCleanWarp = 10;
 constexpr int kThreads = 384;
 constexpr int kHalfBytes = kTile * 64 * 2, kTileBytes = 2 * kHalfBytes;
 constexpr int kRing = 5;
-constexpr int kFlags = 4;                        // items between a flag's uses: more than the ring lets the loads run ahead
+// Items between a flag's uses.  Values of item i + 4 may be looked over before stream 1 has written item i's outputs: of i + 1 to i + 4 it may
+// have no tile, S of i + 2 needs nobody's outputs, and five tiles of the ring hold what comes after its K tile.  So five at least.
+constexpr int kFlags = 8;
 constexpr int kSoftmaxRegs = 216, kOtherRegs = 72;
 static_assert(256 * kSoftmaxRegs + 128 * kOtherRegs <= 65536 / kThreads / 8 * 8 * kThreads, "register shares exceed the launch's");
 constexpr float kRescaleAt = 8.f;                // log2 of the growth of a row's maximum at which its reference follows

@@ -41,3 +41,21 @@ def test_two_streams_of_one_query_tile_both_rescaled(B, n, new, hq, hkv, page, s
     assert p.launches[0]["pairs"] == 0 and p.launches[0]["shares"] == shares
     run_chunk(B, [n], [new], hq, hkv, page, change=rising, seed=n)
     assert B.lookm_last_launch_count() == p.n_launches()
+
+
+@pytest.mark.parametrize("page", [16, 64])
+def test_infinities_in_many_short_items(B, page):
+    """Pairs of query tiles and single ones of one tile of cached rows, several to a CTA, each with an infinity that only its last rows see."""
+    lens = [128] * 40 + [20 + i % 44 for i in range(200)]
+    p = plan_of(lens, lens, 8, 4, page)
+    assert len(p.launches) == 2 and p.launches[0]["units"] > 3 * 128 and p.launches[0]["pairs"] == 160
+    assert not any(x["shares"] for x in p.launches)
+
+    def change(c, q):
+        for r, n in enumerate(lens):
+            v = c.rows(c.v, r, n).float()
+            v[n - 1 - r % 7, r % 4, r % 128] = math.inf if r % 3 else math.nan
+            c.put(c.v, r, 0, v)
+
+    run_chunk(B, lens, lens, 8, 4, page, change=change)
+    assert B.lookm_last_launch_count() == p.n_launches()
