@@ -252,8 +252,8 @@ int lookm_decode_step_varlen(const void* q, const void* k_new, const void* v_new
  *
  * page_table is DEVICE memory, int [n_requests, table_stride]; entries beyond a request's rows are not read.
  * An entry outside 0 .. n_pages - 1 is never followed: the rows of that page are not written (their keys are read as
- * zeros), and lookm_device_status() reports LOOKM_ERR_DEVICE_BAD_INDEX.  Requests may share pages that are
- * only read.
+ * zeros), and lookm_device_status() reports LOOKM_ERR_DEVICE_BAD_INDEX.  Requests may share pages whose
+ * rows are only read (a step adds the weights of all that share them to their masses).
  *
  * The status word: these calls raise it and never clear it, so a problem stays reported until
  * lookm_device_status() has returned it.  Clear a workspace's first 256 bytes before its first use here, and again if
@@ -320,7 +320,9 @@ int lookm_chunk_attention(const void* q, const void* cache_k, const void* cache_
 
 /* The same for one new token per request, which also adds every cached row's softmax weight, summed over the query
  * heads of its KV head, to the row's mass: what lookm_evict goes by.  q, out [n_requests, n_q_heads, 128],
- * lse [n_q_heads, n_requests] or NULL; cache_lens_host: at least 1. */
+ * lse [n_q_heads, n_requests] or NULL; cache_lens_host: at least 1.
+ * Requests that share pages (a prefix in common) all add to these rows' masses, in any order: of such rows, and of no
+ * others, the last bits of the sums may depend on timing. */
 int lookm_step_attention(const void* q, const void* cache_k, const void* cache_v, float* mass, const int* page_table,
                          const int* cache_lens_host, int n_requests, const lookm_paged_layout* paged, void* out,
                          float* lse, void* workspace, size_t workspace_bytes, void* cuda_stream);

@@ -461,14 +461,16 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 }
 
 // Steps: adds the weights of cached rows t, t + stride, ... < end to their mass, summed over the heads of the group; four rows at a time,
-// pages, logits of two heads and masses asked for together.
+// pages and logits of two heads asked for together.  Requests may share pages (a prefix in common) and then add to the same masses: in one atomic
+// operation each, so that nothing is lost.  A mass that one request adds to is that request's alone and doesn't depend on timing; the
+// last bits of a shared one do, as the sharers come in any order.
 __device__ __forceinline__ void add_weights(const ChunkParams& p, int index, int head, int len, const float* logits, const float* lse2, int t,
                                             int end, int stride) {
     const long long row = logits_stride(len);
     const int* table = p.pages.table + (long long)index * p.pages.table_stride;
     for (; t < end; t += 4 * stride) {
         int page[4];
-        float w[4] = {0.f, 0.f, 0.f, 0.f}, m[4], x[2][4];
+        float w[4] = {0.f, 0.f, 0.f, 0.f}, x[2][4];
         const auto ask = [&](int g, float (&y)[4]) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) y[j] = t + j * stride < end ? logits[g * row + t + j * stride] : 0.f;
@@ -482,15 +484,6 @@ __device__ __forceinline__ void add_weights(const ChunkParams& p, int index, int
             page[j] = t + j * stride < end ? __ldg(table + ((t + j * stride) >> p.pages.page_shift)) : 0;
         ask(0, x[0]);
         if (p.group > 1) ask(1, x[1]);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if (page[j] < 0 || page[j] >= p.pages.n_pages) {
-                atomicMax(p.status, (int)LOOKM_ERR_DEVICE_BAD_INDEX);
-                page[j] = -1;
-            }
-            if (t + j * stride >= end) page[j] = -1;
-            m[j] = page[j] >= 0 ? p.mass[p.pages.mass_at(page[j], t + j * stride, head)] : 0.f;
-        }
         for (int g = 0; g < p.group; g += 2) {
             add(g, x[0]);
             if (g + 2 < p.group) ask(g + 2, x[0]);
@@ -498,8 +491,13 @@ __device__ __forceinline__ void add_weights(const ChunkParams& p, int index, int
             if (g + 3 < p.group) ask(g + 3, x[1]);
         }
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (page[j] >= 0) p.mass[p.pages.mass_at(page[j], t + j * stride, head)] = m[j] + w[j];
+        for (int j = 0; j < 4; ++j) {
+            if (t + j * stride >= end) continue;
+            if (page[j] >= 0 && page[j] < p.pages.n_pages)
+                atomicAdd(p.mass + p.pages.mass_at(page[j], t + j * stride, head), w[j]);
+            else
+                atomicMax(p.status, (int)LOOKM_ERR_DEVICE_BAD_INDEX);
+        }
     }
 }
 
