@@ -407,6 +407,8 @@ def make_append_options(q_weight=None, k_weight=None, eps: float = 0.0, inv_freq
                         interleaved: bool = False) -> AppendOptions:
     """Options of lookm_append_rows; the first 2 * len(inv_freq) features are rotated.  The weights are bf16 CUDA tensors [128],
     which the caller keeps alive until the call's work has run."""
+    for w in (q_weight, k_weight):
+        assert w is None or (str(w.dtype) == "torch.bfloat16" and w.is_cuda and w.is_contiguous() and w.numel() == 128)
     freq = None if inv_freq is None else (C.c_double * len(inv_freq))(*[float(x) for x in inv_freq])
     return AppendOptions(_ptr(q_weight), _ptr(k_weight), float(eps), 0 if freq is None else 2 * len(freq), int(bool(interleaved)), freq)
 
@@ -427,11 +429,29 @@ def _here(n: int, page_table, tensors) -> bool:
     return page_table.dtype is _torch.int32 and page_table.shape[0] >= n
 
 
+def _bf16(*tensors) -> bool:
+    for t in tensors:
+        if t is not None and t.dtype is not _torch.bfloat16:
+            return False
+    return True
+
+
+def _dense(t, dtype, n: int) -> bool:
+    """Whether the library, which gets a pointer, can take `t` as n numbers of this type in a row (None is no tensor to look at)."""
+    return t is None or (t.dtype is dtype and t.numel() >= n and t.is_contiguous())
+
+
+def _masses(paged: PagedLayout) -> int:
+    return paged.n_pages * paged.n_kv_heads * paged.page_rows
+
+
 def lookm_append_rows(q, k, v, positions, cu_seqlens, cache_lens, layout: Layout, options, q_out, cache_k, cache_v, mass, page_table,
                       paged: PagedLayout, workspace, stream=None):
-    """options: an AppendOptions (see make_append_options) or None."""
+    """options: an AppendOptions (see make_append_options) or None.  positions: int32."""
     n = len(cache_lens)
-    if len(cu_seqlens) != n + 1 or not _here(n, page_table, (q, k, v, positions, q_out, cache_k, cache_v, mass, page_table, workspace)):
+    if len(cu_seqlens) != n + 1 or not _here(n, page_table, (q, k, v, positions, q_out, cache_k, cache_v, mass, page_table, workspace)) \
+            or not (_bf16(q, k, v, q_out, cache_k, cache_v) and _dense(positions, _torch.int32, cu_seqlens[-1])
+                    and _dense(mass, _torch.float32, _masses(paged))):
         return ERR_INVALID_ARG
     return lib().lookm_append_rows(_ptr(q), _ptr(k), _ptr(v), _ptr(positions), _ints(cu_seqlens), _ints(cache_lens), n,
                                    C.byref(layout), None if options is None else C.byref(options), _ptr(q_out), _ptr(cache_k),
@@ -439,9 +459,15 @@ def lookm_append_rows(q, k, v, positions, cu_seqlens, cache_lens, layout: Layout
                                    _stream(stream))
 
 
+def _results(paged: PagedLayout, tokens: int, out, lse) -> bool:
+    rows = tokens * paged.n_q_heads
+    return _dense(out, _torch.bfloat16, rows * paged.head_dim) and _dense(lse, _torch.float32, rows)
+
+
 def lookm_chunk_attention(q, cache_k, cache_v, page_table, cu_seqlens, cache_lens, paged: PagedLayout, out, lse, workspace, stream=None):
     n = len(cache_lens)
-    if len(cu_seqlens) != n + 1 or not _here(n, page_table, (q, cache_k, cache_v, page_table, out, lse, workspace)):
+    if len(cu_seqlens) != n + 1 or not _here(n, page_table, (q, cache_k, cache_v, page_table, out, lse, workspace)) \
+            or not (_bf16(q, cache_k, cache_v) and _results(paged, cu_seqlens[-1], out, lse)):
         return ERR_INVALID_ARG
     return lib().lookm_chunk_attention(_ptr(q), _ptr(cache_k), _ptr(cache_v), _ptr(page_table), _ints(cu_seqlens), _ints(cache_lens), n,
                                        C.byref(paged), _ptr(out), _ptr(lse), _ptr(workspace), _nbytes(workspace), _stream(stream))
@@ -449,7 +475,8 @@ def lookm_chunk_attention(q, cache_k, cache_v, page_table, cu_seqlens, cache_len
 
 def lookm_step_attention(q, cache_k, cache_v, mass, page_table, cache_lens, paged: PagedLayout, out, lse, workspace, stream=None):
     n = len(cache_lens)
-    if not _here(n, page_table, (q, cache_k, cache_v, mass, page_table, out, lse, workspace)):
+    if not _here(n, page_table, (q, cache_k, cache_v, mass, page_table, out, lse, workspace)) \
+            or not (_bf16(q, cache_k, cache_v) and _results(paged, n, out, lse) and _dense(mass, _torch.float32, _masses(paged))):
         return ERR_INVALID_ARG
     return lib().lookm_step_attention(_ptr(q), _ptr(cache_k), _ptr(cache_v), _ptr(mass), _ptr(page_table), _ints(cache_lens), n,
                                       C.byref(paged), _ptr(out), _ptr(lse), _ptr(workspace), _nbytes(workspace), _stream(stream))
@@ -461,7 +488,11 @@ def lookm_evict(cache_k, cache_v, mass, page_table, cache_lens, budgets, windows
     if len(budgets) != n or len(windows) != n or not _here(n, page_table, (cache_k, cache_v, mass, page_table, out_k, out_v, out_mass,
                                                                            out_page_table, kept_idx, workspace)) \
             or out_page_table.dtype is not page_table.dtype or out_page_table.shape[0] < n \
-            or (n > 1 and out_page_table.stride(0) != page_table.stride(0)):
+            or (n > 1 and out_page_table.stride(0) != page_table.stride(0)) or not _bf16(cache_k, cache_v, out_k, out_v):
+        return ERR_INVALID_ARG
+    masses = _masses(paged)
+    if not (_dense(mass, _torch.float32, masses) and _dense(out_mass, _torch.float32, masses) and
+            (kept_idx is None or _dense(kept_idx, _torch.int32, paged.n_kv_heads * sum(map(min, budgets, cache_lens))))):
         return ERR_INVALID_ARG
     return lib().lookm_evict(_ptr(cache_k), _ptr(cache_v), _ptr(mass), _ptr(page_table), _ints(cache_lens), _ints(budgets),
                              _ints(windows), n, C.byref(paged), _ptr(out_k), _ptr(out_v), _ptr(out_mass),
