@@ -416,9 +416,8 @@ def make_append_options(q_weight=None, k_weight=None, eps: float = 0.0, inv_freq
 _torch = None                                    # imported when first needed
 
 
-def _here(n: int, page_table, tensors) -> bool:
-    """Whether all tensors are on the current device, where the call would run, and the table has a row for each of the n requests
-    (the library reads it by pointer and can't tell)."""
+def _here(tensors) -> bool:
+    """Whether all tensors are on the current device, where the call would run."""
     global _torch
     if _torch is None:
         import torch as _torch
@@ -426,7 +425,19 @@ def _here(n: int, page_table, tensors) -> bool:
     for t in tensors:
         if t is not None and t.get_device() != dev:
             return False
-    return page_table.dtype is _torch.int32 and page_table.shape[0] >= n
+    return True
+
+
+def _table(t, paged: PagedLayout, lens, more=None) -> bool:
+    """Whether `t` holds page numbers, as the layout has it, for len(lens) requests of these many rows (and `more` of them: cu_seqlens)."""
+    if t.dtype is not _torch.int32 or t.dim() != 2:
+        return False
+    (rows, cols), (row_stride, stride), n = t.shape, t.stride(), len(lens)
+    if rows < n or (n > 1 and row_stride != paged.table_stride) or (cols > 1 and stride != 1):
+        return False
+    # fewer columns than the layout's rows are long (what the library looks at): enough all the same for these requests?
+    return cols >= paged.table_stride or max(lens if more is None else [a + more[i + 1] - more[i] for i, a in enumerate(lens)],
+                                             default=0) <= cols * paged.page_rows
 
 
 def _bf16(*tensors) -> bool:
@@ -449,9 +460,9 @@ def lookm_append_rows(q, k, v, positions, cu_seqlens, cache_lens, layout: Layout
                       paged: PagedLayout, workspace, stream=None):
     """options: an AppendOptions (see make_append_options) or None.  positions: int32."""
     n = len(cache_lens)
-    if len(cu_seqlens) != n + 1 or not _here(n, page_table, (q, k, v, positions, q_out, cache_k, cache_v, mass, page_table, workspace)) \
-            or not (_bf16(q, k, v, q_out, cache_k, cache_v) and _dense(positions, _torch.int32, cu_seqlens[-1])
-                    and _dense(mass, _torch.float32, _masses(paged))):
+    if len(cu_seqlens) != n + 1 or not _here((q, k, v, positions, q_out, cache_k, cache_v, mass, page_table, workspace)) \
+            or not (_table(page_table, paged, cache_lens, cu_seqlens) and _bf16(q, k, v, q_out, cache_k, cache_v)
+                    and _dense(positions, _torch.int32, cu_seqlens[-1]) and _dense(mass, _torch.float32, _masses(paged))):
         return ERR_INVALID_ARG
     return lib().lookm_append_rows(_ptr(q), _ptr(k), _ptr(v), _ptr(positions), _ints(cu_seqlens), _ints(cache_lens), n,
                                    C.byref(layout), None if options is None else C.byref(options), _ptr(q_out), _ptr(cache_k),
@@ -466,8 +477,8 @@ def _results(paged: PagedLayout, tokens: int, out, lse) -> bool:
 
 def lookm_chunk_attention(q, cache_k, cache_v, page_table, cu_seqlens, cache_lens, paged: PagedLayout, out, lse, workspace, stream=None):
     n = len(cache_lens)
-    if len(cu_seqlens) != n + 1 or not _here(n, page_table, (q, cache_k, cache_v, page_table, out, lse, workspace)) \
-            or not (_bf16(q, cache_k, cache_v) and _results(paged, cu_seqlens[-1], out, lse)):
+    if len(cu_seqlens) != n + 1 or not _here((q, cache_k, cache_v, page_table, out, lse, workspace)) \
+            or not (_table(page_table, paged, cache_lens) and _bf16(q, cache_k, cache_v) and _results(paged, cu_seqlens[-1], out, lse)):
         return ERR_INVALID_ARG
     return lib().lookm_chunk_attention(_ptr(q), _ptr(cache_k), _ptr(cache_v), _ptr(page_table), _ints(cu_seqlens), _ints(cache_lens), n,
                                        C.byref(paged), _ptr(out), _ptr(lse), _ptr(workspace), _nbytes(workspace), _stream(stream))
@@ -475,8 +486,9 @@ def lookm_chunk_attention(q, cache_k, cache_v, page_table, cu_seqlens, cache_len
 
 def lookm_step_attention(q, cache_k, cache_v, mass, page_table, cache_lens, paged: PagedLayout, out, lse, workspace, stream=None):
     n = len(cache_lens)
-    if not _here(n, page_table, (q, cache_k, cache_v, mass, page_table, out, lse, workspace)) \
-            or not (_bf16(q, cache_k, cache_v) and _results(paged, n, out, lse) and _dense(mass, _torch.float32, _masses(paged))):
+    if not _here((q, cache_k, cache_v, mass, page_table, out, lse, workspace)) \
+            or not (_table(page_table, paged, cache_lens) and _bf16(q, cache_k, cache_v) and _results(paged, n, out, lse)
+                    and _dense(mass, _torch.float32, _masses(paged))):
         return ERR_INVALID_ARG
     return lib().lookm_step_attention(_ptr(q), _ptr(cache_k), _ptr(cache_v), _ptr(mass), _ptr(page_table), _ints(cache_lens), n,
                                       C.byref(paged), _ptr(out), _ptr(lse), _ptr(workspace), _nbytes(workspace), _stream(stream))
@@ -485,14 +497,13 @@ def lookm_step_attention(q, cache_k, cache_v, mass, page_table, cache_lens, page
 def lookm_evict(cache_k, cache_v, mass, page_table, cache_lens, budgets, windows, paged: PagedLayout, out_k, out_v, out_mass,
                 out_page_table, kept_idx, workspace, stream=None):
     n = len(cache_lens)
-    if len(budgets) != n or len(windows) != n or not _here(n, page_table, (cache_k, cache_v, mass, page_table, out_k, out_v, out_mass,
-                                                                           out_page_table, kept_idx, workspace)) \
-            or out_page_table.dtype is not page_table.dtype or out_page_table.shape[0] < n \
-            or (n > 1 and out_page_table.stride(0) != page_table.stride(0)) or not _bf16(cache_k, cache_v, out_k, out_v):
+    if len(budgets) != n or len(windows) != n or not _here((cache_k, cache_v, mass, page_table, out_k, out_v, out_mass, out_page_table,
+                                                            kept_idx, workspace)) \
+            or not (_table(page_table, paged, cache_lens) and _bf16(cache_k, cache_v, out_k, out_v)):
         return ERR_INVALID_ARG
-    masses = _masses(paged)
-    if not (_dense(mass, _torch.float32, masses) and _dense(out_mass, _torch.float32, masses) and
-            (kept_idx is None or _dense(kept_idx, _torch.int32, paged.n_kv_heads * sum(map(min, budgets, cache_lens))))):
+    masses, kept = _masses(paged), list(map(min, budgets, cache_lens))
+    if not (_table(out_page_table, paged, kept) and _dense(mass, _torch.float32, masses) and _dense(out_mass, _torch.float32, masses) and
+            _dense(kept_idx, _torch.int32, paged.n_kv_heads * sum(kept))):
         return ERR_INVALID_ARG
     return lib().lookm_evict(_ptr(cache_k), _ptr(cache_v), _ptr(mass), _ptr(page_table), _ints(cache_lens), _ints(budgets),
                              _ints(windows), n, C.byref(paged), _ptr(out_k), _ptr(out_v), _ptr(out_mass),

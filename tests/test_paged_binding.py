@@ -128,3 +128,25 @@ def test_weights_of_the_norm():
             B.make_append_options(bad, None, 1e-6)
         with pytest.raises(AssertionError):
             B.make_append_options(None, bad, 1e-6)
+
+
+@pytest.mark.parametrize("call", CALLS)
+def test_tables_that_are_not_the_layouts(library, call):
+    """The library goes by the layout's stride: entries of other requests, or what lies behind the table, would be taken for page numbers."""
+    names = ["page_table"] + (["out_page_table"] if call == "evict" else [])
+    wide, one = torch.zeros(2, 6, dtype=torch.int32), dict(lens=LENS[1:], **{"append": dict(cu=[0, 5]), "chunk": dict(cu=[0, 5]), "step": {},
+                                                                             "evict": dict(budgets=[30], windows=[1])}[call])
+    last = LENS[1] + (5 if call == "append" else 0)          # rows of a single request's cache: three pages
+    assert 2 * PAGE < last <= 3 * PAGE
+    for name in names:
+        refused(library, call, **{name: wide})               # it has grown since the layout was made
+        refused(library, call, **{name: wide[:, :4].contiguous()[:1]})
+        refused(library, call, **{name: torch.zeros(4, 2, dtype=torch.int32).t()})
+        refused(library, call, **{name: torch.zeros(8, dtype=torch.int32)})
+        refused(library, call, **{name: table()[:, :2] if name == "page_table" else table()[:, :1]})
+        taken(library, call, **{name: wide[:1]}, **one)      # one request: no other row is looked for
+        taken(library, call, **{name: torch.zeros(1, 3, dtype=torch.int32)}, **one)          # fewer columns, and enough
+        refused(library, call, **{name: torch.zeros(1, 2 if name == "page_table" else 1, dtype=torch.int32)}, **one)
+    both = torch.zeros(2, 10, dtype=torch.int32)[:, :4]      # (a stride that is not the number of columns)
+    a = arguments(call)
+    taken(library, call, **{name: both for name in names}, paged=B.make_paged_layout(a.get("q"), a["cache_k"], both, n_q_heads=HQ))
