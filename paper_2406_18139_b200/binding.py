@@ -166,12 +166,22 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+_torch = _BF16 = _F32 = _I32 = None              # imported when first needed
+
+
+def _import_torch():
+    global _torch, _BF16, _F32, _I32
+    import torch
+    _torch, _BF16, _F32, _I32 = torch, torch.bfloat16, torch.float32, torch.int32
+
+
 def _stream(stream) -> int:
     """The raw handle of `stream`, or of PyTorch's current stream on the current device (asked for
     directly: building a torch.cuda.Stream object takes longer than a small call)."""
     if stream is None:
-        import torch
-        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+        if _torch is None:
+            _import_torch()
+        return _torch._C._cuda_getCurrentRawStream(_torch._C._cuda_getDevice())
     return stream.cuda_stream
 
 
@@ -413,14 +423,11 @@ def make_append_options(q_weight=None, k_weight=None, eps: float = 0.0, inv_freq
     return AppendOptions(_ptr(q_weight), _ptr(k_weight), float(eps), 0 if freq is None else 2 * len(freq), int(bool(interleaved)), freq)
 
 
-_torch = None                                    # imported when first needed
-
-
+# What follows is looked at in every call, of which the shortest take some microseconds: usual cases come first.
 def _here(tensors) -> bool:
     """Whether all tensors are on the current device, where the call would run."""
-    global _torch
     if _torch is None:
-        import torch as _torch
+        _import_torch()
     dev = _torch._C._cuda_getDevice()
     for t in tensors:
         if t is not None and t.get_device() != dev:
@@ -428,23 +435,28 @@ def _here(tensors) -> bool:
     return True
 
 
-def _table(t, paged: PagedLayout, lens, more=None) -> bool:
-    """Whether `t` holds page numbers, as the layout has it, for len(lens) requests of these many rows (and `more` of them: cu_seqlens)."""
-    if t.dtype is not _torch.int32 or t.dim() != 2:
+def _table(t, paged: PagedLayout, n: int, lens, more=None) -> bool:
+    """Whether `t` holds page numbers, as the layout has it, for n requests of these many rows (and `more` of them: cu_seqlens)."""
+    if t.dtype is not _I32:
         return False
-    (rows, cols), (row_stride, stride), n = t.shape, t.stride(), len(lens)
-    if rows < n or (n > 1 and row_stride != paged.table_stride) or (cols > 1 and stride != 1):
+    stride = paged.table_stride
+    if t.stride() == (stride, 1) and t.nbytes >= 4 * n * stride and t.shape[1] == stride:
+        return True
+    if t.dim() != 2 or t.shape[0] < n or (n > 1 and t.stride(0) != stride) or (t.shape[1] > 1 and t.stride(1) != 1):
         return False
     # fewer columns than the layout's rows are long (what the library looks at): enough all the same for these requests?
-    return cols >= paged.table_stride or max(lens if more is None else [a + more[i + 1] - more[i] for i, a in enumerate(lens)],
-                                             default=0) <= cols * paged.page_rows
+    return t.shape[1] >= stride or max(lens if more is None else [a + more[i + 1] - more[i] for i, a in enumerate(lens)],
+                                       default=0) <= t.shape[1] * paged.page_rows
 
 
-def _bf16(*tensors) -> bool:
-    for t in tensors:
-        if t is not None and t.dtype is not _torch.bfloat16:
-            return False
-    return True
+def _strided(t, shape, strides) -> bool:
+    """Whether `t` is bf16 of this shape, or with more in the first dimension, and with these strides."""
+    if t is None or t.dtype is not _BF16:
+        return False
+    if t.shape == shape and t.stride() == strides:
+        return True
+    return t.dim() == len(shape) and t.shape[0] >= shape[0] and t.shape[1:] == shape[1:] and \
+        all(a == b for a, b, n in zip(t.stride(), strides, shape) if n > 1)          # (a dimension of one may have any stride)
 
 
 def _dense(t, dtype, n: int) -> bool:
@@ -452,62 +464,77 @@ def _dense(t, dtype, n: int) -> bool:
     return t is None or (t.dtype is dtype and t.numel() >= n and t.is_contiguous())
 
 
-def _masses(paged: PagedLayout) -> int:
-    return paged.n_pages * paged.n_kv_heads * paged.page_rows
-
-
 def lookm_append_rows(q, k, v, positions, cu_seqlens, cache_lens, layout: Layout, options, q_out, cache_k, cache_v, mass, page_table,
                       paged: PagedLayout, workspace, stream=None):
     """options: an AppendOptions (see make_append_options) or None.  positions: int32."""
     n = len(cache_lens)
-    if len(cu_seqlens) != n + 1 or not _here((q, k, v, positions, q_out, cache_k, cache_v, mass, page_table, workspace)) \
-            or not (_table(page_table, paged, cache_lens, cu_seqlens) and _bf16(q, k, v, q_out, cache_k, cache_v)
-                    and _dense(positions, _torch.int32, cu_seqlens[-1]) and _dense(mass, _torch.float32, _masses(paged))):
+    if len(cu_seqlens) != n + 1 or not _here((q, k, v, positions, q_out, cache_k, cache_v, mass, page_table, workspace)):
         return ERR_INVALID_ARG
-    return lib().lookm_append_rows(_ptr(q), _ptr(k), _ptr(v), _ptr(positions), _ints(cu_seqlens), _ints(cache_lens), n,
-                                   C.byref(layout), None if options is None else C.byref(options), _ptr(q_out), _ptr(cache_k),
-                                   _ptr(cache_v), _ptr(mass), _ptr(page_table), C.byref(paged), _ptr(workspace), _nbytes(workspace),
-                                   _stream(stream))
+    tokens, dim, hkv = cu_seqlens[-1], paged.head_dim, paged.n_kv_heads
+    rows, row_strides = (tokens, hkv, dim), (layout.kv_stride_tok, layout.kv_stride_head, 1)
+    pages, page_strides = (paged.n_pages, hkv, paged.page_rows, dim), (paged.page_stride, paged.head_stride, paged.row_stride, 1)
+    if not (_strided(k, rows, row_strides) and _strided(v, rows, row_strides) and _strided(cache_k, pages, page_strides)
+            and _strided(cache_v, pages, page_strides) and _table(page_table, paged, n, cache_lens, cu_seqlens)
+            and _dense(positions, _I32, tokens) and _dense(mass, _F32, pages[0] * hkv * pages[2])):
+        return ERR_INVALID_ARG
+    if q is not None:
+        rows = (tokens, paged.n_q_heads, dim)
+        if not (_strided(q, rows, (layout.q_stride_tok, layout.q_stride_head, 1)) and
+                _strided(q_out, rows, (paged.q_stride_tok, paged.q_stride_head, 1))):
+            return ERR_INVALID_ARG
+    return lib().lookm_append_rows(_ptr(q), k.data_ptr(), v.data_ptr(), _ptr(positions), _ints(cu_seqlens), _ints(cache_lens), n,
+                                   C.byref(layout), None if options is None else C.byref(options), _ptr(q_out), cache_k.data_ptr(),
+                                   cache_v.data_ptr(), _ptr(mass), page_table.data_ptr(), C.byref(paged), workspace.data_ptr(),
+                                   workspace.nbytes, _stream(stream))
 
 
-def _results(paged: PagedLayout, tokens: int, out, lse) -> bool:
-    rows = tokens * paged.n_q_heads
-    return _dense(out, _torch.bfloat16, rows * paged.head_dim) and _dense(lse, _torch.float32, rows)
+def _attention(paged: PagedLayout, n: int, lens, tokens: int, q, cache_k, cache_v, mass, page_table, out, lse) -> bool:
+    """Whether these tensors are what attention of `tokens` rows of queries over n caches takes."""
+    dim, hq, hkv = paged.head_dim, paged.n_q_heads, paged.n_kv_heads
+    pages, page_strides = (paged.n_pages, hkv, paged.page_rows, dim), (paged.page_stride, paged.head_stride, paged.row_stride, 1)
+    return _strided(q, (tokens, hq, dim), (paged.q_stride_tok, paged.q_stride_head, 1)) and _strided(cache_k, pages, page_strides) \
+        and _strided(cache_v, pages, page_strides) and _table(page_table, paged, n, lens) \
+        and _dense(out, _BF16, tokens * hq * dim) and _dense(lse, _F32, tokens * hq) \
+        and _dense(mass, _F32, pages[0] * hkv * pages[2])
 
 
 def lookm_chunk_attention(q, cache_k, cache_v, page_table, cu_seqlens, cache_lens, paged: PagedLayout, out, lse, workspace, stream=None):
     n = len(cache_lens)
     if len(cu_seqlens) != n + 1 or not _here((q, cache_k, cache_v, page_table, out, lse, workspace)) \
-            or not (_table(page_table, paged, cache_lens) and _bf16(q, cache_k, cache_v) and _results(paged, cu_seqlens[-1], out, lse)):
+            or not _attention(paged, n, cache_lens, cu_seqlens[-1], q, cache_k, cache_v, None, page_table, out, lse):
         return ERR_INVALID_ARG
-    return lib().lookm_chunk_attention(_ptr(q), _ptr(cache_k), _ptr(cache_v), _ptr(page_table), _ints(cu_seqlens), _ints(cache_lens), n,
-                                       C.byref(paged), _ptr(out), _ptr(lse), _ptr(workspace), _nbytes(workspace), _stream(stream))
+    return lib().lookm_chunk_attention(q.data_ptr(), cache_k.data_ptr(), cache_v.data_ptr(), page_table.data_ptr(), _ints(cu_seqlens),
+                                       _ints(cache_lens), n, C.byref(paged), _ptr(out), _ptr(lse), workspace.data_ptr(), workspace.nbytes,
+                                       _stream(stream))
 
 
 def lookm_step_attention(q, cache_k, cache_v, mass, page_table, cache_lens, paged: PagedLayout, out, lse, workspace, stream=None):
     n = len(cache_lens)
     if not _here((q, cache_k, cache_v, mass, page_table, out, lse, workspace)) \
-            or not (_table(page_table, paged, cache_lens) and _bf16(q, cache_k, cache_v) and _results(paged, n, out, lse)
-                    and _dense(mass, _torch.float32, _masses(paged))):
+            or not _attention(paged, n, cache_lens, n, q, cache_k, cache_v, mass, page_table, out, lse):
         return ERR_INVALID_ARG
-    return lib().lookm_step_attention(_ptr(q), _ptr(cache_k), _ptr(cache_v), _ptr(mass), _ptr(page_table), _ints(cache_lens), n,
-                                      C.byref(paged), _ptr(out), _ptr(lse), _ptr(workspace), _nbytes(workspace), _stream(stream))
+    return lib().lookm_step_attention(q.data_ptr(), cache_k.data_ptr(), cache_v.data_ptr(), _ptr(mass), page_table.data_ptr(),
+                                      _ints(cache_lens), n, C.byref(paged), _ptr(out), _ptr(lse), workspace.data_ptr(), workspace.nbytes,
+                                      _stream(stream))
 
 
 def lookm_evict(cache_k, cache_v, mass, page_table, cache_lens, budgets, windows, paged: PagedLayout, out_k, out_v, out_mass,
                 out_page_table, kept_idx, workspace, stream=None):
     n = len(cache_lens)
     if len(budgets) != n or len(windows) != n or not _here((cache_k, cache_v, mass, page_table, out_k, out_v, out_mass, out_page_table,
-                                                            kept_idx, workspace)) \
-            or not (_table(page_table, paged, cache_lens) and _bf16(cache_k, cache_v, out_k, out_v)):
+                                                            kept_idx, workspace)):
         return ERR_INVALID_ARG
-    masses, kept = _masses(paged), list(map(min, budgets, cache_lens))
-    if not (_table(out_page_table, paged, kept) and _dense(mass, _torch.float32, masses) and _dense(out_mass, _torch.float32, masses) and
-            _dense(kept_idx, _torch.int32, paged.n_kv_heads * sum(kept))):
+    hkv, kept = paged.n_kv_heads, list(map(min, budgets, cache_lens))
+    pages, page_strides = (paged.n_pages, hkv, paged.page_rows, paged.head_dim), (paged.page_stride, paged.head_stride, paged.row_stride, 1)
+    masses = pages[0] * hkv * pages[2]
+    if not (_strided(cache_k, pages, page_strides) and _strided(cache_v, pages, page_strides) and _strided(out_k, pages, page_strides)
+            and _strided(out_v, pages, page_strides) and _table(page_table, paged, n, cache_lens) and _table(out_page_table, paged, n, kept)
+            and _dense(mass, _F32, masses) and _dense(out_mass, _F32, masses)
+            and _dense(kept_idx, _I32, hkv * sum(kept))):
         return ERR_INVALID_ARG
-    return lib().lookm_evict(_ptr(cache_k), _ptr(cache_v), _ptr(mass), _ptr(page_table), _ints(cache_lens), _ints(budgets),
-                             _ints(windows), n, C.byref(paged), _ptr(out_k), _ptr(out_v), _ptr(out_mass),
-                             _ptr(out_page_table), _ptr(kept_idx), _ptr(workspace), _nbytes(workspace), _stream(stream))
+    return lib().lookm_evict(cache_k.data_ptr(), cache_v.data_ptr(), _ptr(mass), page_table.data_ptr(), _ints(cache_lens), _ints(budgets),
+                             _ints(windows), n, C.byref(paged), out_k.data_ptr(), out_v.data_ptr(), _ptr(out_mass),
+                             out_page_table.data_ptr(), _ptr(kept_idx), workspace.data_ptr(), workspace.nbytes, _stream(stream))
 
 
 _stage_event_array = None

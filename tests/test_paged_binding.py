@@ -150,3 +150,64 @@ def test_tables_that_are_not_the_layouts(library, call):
     both = torch.zeros(2, 10, dtype=torch.int32)[:, :4]      # (a stride that is not the number of columns)
     a = arguments(call)
     taken(library, call, **{name: both for name in names}, paged=B.make_paged_layout(a.get("q"), a["cache_k"], both, n_q_heads=HQ))
+
+
+def apart(t):
+    """The same numbers with a gap behind every first index."""
+    wide = torch.zeros(t.shape[0], 2, *t.shape[1:], dtype=t.dtype)
+    wide[:, 0] = t
+    return wide[:, 0]
+
+
+POOLS = {"append": ["cache_k", "cache_v"], "chunk": ["cache_k", "cache_v"], "step": ["cache_k", "cache_v"],
+         "evict": ["cache_k", "cache_v", "out_k", "out_v"]}
+
+
+@pytest.mark.parametrize("call", CALLS)
+def test_pools_that_are_not_the_layouts(library, call):
+    """One layout stands for all pools of a call: another pool's strides would be taken for its own."""
+    more = torch.zeros(PAGES + 2, HKV, PAGE, 128, dtype=bf16)
+    for name in POOLS[call]:
+        refused(library, call, **{name: torch.zeros(PAGES, PAGE, HKV, 128, dtype=bf16).transpose(1, 2)})
+        refused(library, call, **{name: apart(pool())})
+        refused(library, call, **{name: pool()[:-1]})
+        refused(library, call, **{name: torch.zeros(PAGES, 2 * HKV, PAGE, 128, dtype=bf16)[:, :HKV]})
+        refused(library, call, **{name: torch.zeros(PAGES, HKV, 128, PAGE, dtype=bf16).transpose(2, 3)})
+        refused(library, call, **{name: None})
+        taken(library, call, **{name: more})                 # further pages that no table names
+    rows_first = {name: torch.zeros(PAGES, PAGE, HKV, 128, dtype=bf16).transpose(1, 2) for name in POOLS[call]}
+    a = arguments(call)
+    taken(library, call, **rows_first, paged=B.make_paged_layout(a.get("q"), rows_first["cache_k"], a["page_table"], n_q_heads=HQ))
+    # a dimension of one may have any stride
+    one = {name: torch.zeros(PAGES, 3, PAGE, 128, dtype=bf16)[:, :1] for name in POOLS[call]}
+    same = {name: torch.zeros(PAGES, 1, PAGE, 128, dtype=bf16).expand(PAGES, 1, PAGE, 128) for name in POOLS[call]}
+    if call in ("chunk", "step"):
+        taken(library, call, **one, paged=B.make_paged_layout(a["q"], one["cache_k"], a["page_table"]))
+        refused(library, call, **same, paged=B.make_paged_layout(a["q"], one["cache_k"], a["page_table"]))
+
+
+@pytest.mark.parametrize("call,names", [("append", ["q", "k", "v", "q_out"]), ("chunk", ["q"]), ("step", ["q"])])
+def test_rows_of_new_tokens_that_are_not_the_layouts(library, call, names):
+    a = arguments(call)
+    for name in names:
+        t = a[name]
+        refused(library, call, **{name: apart(t)})
+        refused(library, call, **{name: t[:-1]})
+        refused(library, call, **{name: torch.cat([t, t], dim=1)})
+        refused(library, call, **{name: torch.cat([t, t], dim=1)[:, ::2]})
+        refused(library, call, **{name: t.reshape(len(t), -1)})
+        taken(library, call, **{name: torch.cat([t, t])})
+        if name in ("k", "v"):
+            refused(library, call, **{name: None})
+    if call == "append":                                     # one buffer of q, k and v, as a fused projection leaves it
+        q, k, v = rows(HQ + 2 * HKV).split([HQ, HKV, HKV], dim=1)
+        taken(library, call, q=q, k=k, v=v, layout=B.make_layout(q, k))
+        refused(library, call, q=q, k=k, layout=B.make_layout(q, k))                       # (v lies otherwise)
+
+
+def test_a_single_token_may_have_any_stride(library):
+    a = arguments("append")
+    q, k, v = rows(HQ + 2 * HKV, 1).split([HQ, HKV, HKV], dim=1)
+    taken(library, "append", q=q, k=k, v=rows(HKV, 1), q_out=rows(HQ, 7)[:1], cu=[0, 1, 1], layout=B.make_layout(q, k))
+    taken(library, "chunk", q=rows(2 * HQ, 1)[:, :HQ], cu=[0, 1, 1])
+    taken(library, "chunk", q=a["q"][:0], cu=[0, 0, 0])
