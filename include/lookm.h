@@ -296,7 +296,7 @@ typedef struct {
  *   q, k, v     [tokens, heads, 128] bf16 with the strides of `layout`; q and q_out may both be NULL
  *   positions   device [tokens], may be NULL if rotary_dim is 0
  *   q_out       the normed and rotated queries, with the q strides of `paged`.  May be q itself if the
- *               strides are the same; other outputs must not overlap inputs
+ *               strides are the same (else LOOKM_ERR_INVALID_ARG); other outputs must not overlap inputs
  *   mass        set to 0 for the new rows; may be NULL */
 int lookm_append_rows(const void* q, const void* k, const void* v, const int* positions, const int* cu_seqlens_host,
                       const int* cache_lens_host, int n_requests, const lookm_layout* layout,

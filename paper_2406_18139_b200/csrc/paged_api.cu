@@ -115,6 +115,10 @@ int append_rows(const void* q, const void* k, const void* v, const int* position
     if (q)
         for (long long s : {lay->q_stride_tok, lay->q_stride_head, paged->q_stride_tok, paged->q_stride_head})
             if (s <= 0 || s % 8) return LOOKM_ERR_INVALID_ARG;
+    // in place, a row would otherwise be written where another one is still to be read
+    if (q && q == q_out && ((cu[n] > 1 && lay->q_stride_tok != paged->q_stride_tok) ||
+                            (paged->n_q_heads > 1 && lay->q_stride_head != paged->q_stride_head)))
+        return LOOKM_ERR_INVALID_ARG;
     AppendParams p;
     p.q_weight = opt ? opt->q_weight : nullptr;
     p.k_weight = opt ? opt->k_weight : nullptr;
