@@ -78,3 +78,55 @@ def test_a_page_that_a_request_names_twice(B):
     w, tol_w = (x[:, 0].sum(0) for x in (w, tol_w))
     got = c.mass[c.table[0, 0], 0].double() - old[c.table[0, 0], 0].double()
     assert ((got - w[:16] - w[32:48]).abs() <= tol_w[:16] + tol_w[32:48] + 2.0 ** -24 * 6 * c.mass[c.table[0, 0], 0].abs()).all()
+
+
+def check(B, c, q, hq, hkv, out, lse, old, scale):
+    """Outputs, log-sum-exps and masses of a step, against fp64."""
+    for r, k in enumerate(c.lens):
+        ref, ref_lse, w, tol, tol_lse, tol_w = reference(c, r, q[r:r + 1], 1, scale)
+        assert close(out[r:r + 1], ref, tol), r
+        assert close(lse[:, r:r + 1], ref_lse, tol_lse), r
+        p, o = c.where(r, 0, k)
+        sums, tols = (x[:, 0].view(hkv, hq // hkv, k).sum(1).t() for x in (w, tol_w))
+        ref_m = old[p, :, o].double() + sums
+        assert close(c.mass[p, :, o], ref_m, tols + 2.0 ** -23 * (hq // hkv + 1) * ref_m.abs()), r
+
+
+@pytest.mark.parametrize("scale", [0.02, 0.3])
+@pytest.mark.parametrize("lens,hq,hkv,page", [([5, 700], 8, 2, 16), ([9000], 4, 4, 64), ([70000], 2, 1, 65536)])
+def test_scales(B, scale, lens, hq, hkv, page):
+    c = Cache(lens, hkv, page, sum(lens))
+    q, lse, old = c.normal(len(lens), hq, D).bfloat16(), torch.empty(hq, len(lens), device="cuda"), c.mass.clone()
+    out = step(B, c, q, hq, lse, scale)
+    check(B, c, q, hq, hkv, out, lse, old, scale)
+
+
+@pytest.mark.parametrize("n,hq,hkv,page", [(129, 4, 4, 16), (1500, 8, 2, 16), (9000, 8, 2, 16), (4000, 2, 1, 64)])
+@pytest.mark.parametrize("kind", ["v nan", "v inf", "k nan", "k -inf", "k all -inf"])
+def test_infinities_and_nan(B, n, hq, hkv, page, kind):
+    """What a row holds reaches the outputs and the masses of its head, and no other head's."""
+    c = Cache([n], hkv, page, n)
+    q = c.normal(1, hq, D).bfloat16()
+    k, v = c.rows(c.k, 0, n).float(), c.rows(c.v, 0, n).float()
+    if kind == "v nan":
+        v[n - 1, 0, 5] = math.nan
+    elif kind == "v inf":
+        v[n - 1, -1, 0], v[0, 0, 77], v[n // 2, 0, 77], v[n // 2, 0, 3] = math.inf, -math.inf, math.inf, math.inf
+    elif kind == "k nan":
+        k[n // 2, 0, 9] = math.nan
+    else:
+        q[..., 4] = 1.0
+        k[(slice(None) if "all" in kind else n // 3), 0, 4] = -math.inf
+    c.put(c.k, 0, 0, k)
+    c.put(c.v, 0, 0, v)
+    lse, old = torch.empty(hq, 1, device="cuda"), c.mass.clone()
+    out = step(B, c, q, hq, lse)
+    check(B, c, q, hq, hkv, out, lse, old, D ** -0.5)
+
+
+@pytest.mark.parametrize("lens", [[9000 + 400 * (i % 9) for i in range(140)], [300 + i for i in range(300)]])
+def test_more_requests_than_a_launch_takes(B, lens):
+    c = Cache(lens, 1, 32, 21)
+    q, lse, old = c.normal(len(lens), 2, D).bfloat16(), torch.empty(2, len(lens), device="cuda"), c.mass.clone()
+    out = step(B, c, q, 2, lse)
+    check(B, c, q, 2, 1, out, lse, old, D ** -0.5)
