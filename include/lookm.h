@@ -247,13 +247,16 @@ int lookm_decode_step_varlen(const void* q, const void* k_new, const void* v_new
  * of either pool: [n_pages, n_kv_heads, page_rows, 128] and [n_pages, page_rows, n_kv_heads, 128] pools, or
  * runs of pages inside a [n_kv_heads, capacity, 128] buffer, into which lookm_compress_layer_opt can write
  * (lookm_options.out_stride_head).  `mass` is fp32 [n_pages, n_kv_heads, page_rows], contiguous: the attention
- * weight that every cached row has received.  Strides are multiples of 8 elements, at least 128; pools,
+ * weight that every cached row has received from steps.  Strides are multiples of 8 elements, at least 128; pools,
  * queries and outputs are 16-byte aligned.
  *
  * page_table is DEVICE memory, int [n_requests, table_stride]; entries beyond a request's rows are not read.
  * An entry outside 0 .. n_pages - 1 is never followed: the rows of that page are not written (their keys are read as
  * zeros), and lookm_device_status() reports LOOKM_ERR_DEVICE_BAD_INDEX.  Requests may share pages whose
  * rows are only read (a step adds the weights of all that share them to their masses).
+ *
+ * Lengths, first rows and what follows from them travel with the launches: a captured call repeats the lengths that it was
+ * captured with.
  *
  * The status word: these calls raise it and never clear it, so a problem stays reported until
  * lookm_device_status() has returned it.  Clear a workspace's first 256 bytes before its first use here, and again if
@@ -297,7 +300,9 @@ typedef struct {
  *   positions   device [tokens], may be NULL if rotary_dim is 0
  *   q_out       the normed and rotated queries, with the q strides of `paged`.  May be q itself if the
  *               strides are the same (else LOOKM_ERR_INVALID_ARG); other outputs must not overlap inputs
- *   mass        set to 0 for the new rows; may be NULL */
+ *   mass        set to 0 for the new rows; may be NULL.  Of the calls below only lookm_step_attention adds to it: what the
+ *               tokens of a prompt or of a further turn attend to is counted nowhere, so before an eviction right after
+ *               one a caller gives such rows masses of its own or a window that holds them */
 int lookm_append_rows(const void* q, const void* k, const void* v, const int* positions, const int* cu_seqlens_host,
                       const int* cache_lens_host, int n_requests, const lookm_layout* layout,
                       const lookm_append_options* options, void* q_out, void* cache_k, void* cache_v, float* mass,
@@ -312,6 +317,9 @@ int lookm_append_rows(const void* q, const void* k, const void* v, const int* po
  *   out   [tokens, n_q_heads, 128] bf16, contiguous
  *   lse   [n_q_heads, tokens] fp32, natural-log row log-sum-exp; may be NULL
  *   cache_lens_host  rows of each cache with the new ones: at least as many as the new tokens
+ * Logits, the softmax's maximum and sum, and the sums over the rows are fp32; probabilities are rounded to bf16 (2^-8 of each at most) for the
+ * product with V, the result to bf16 once more.  Against 64 bits the two together are off by 2.2e-3 of the result's norm where values are
+ * independent, the last rounding alone by 1.7e-3.  lse and a step's weights have no part in either.
  * Results do not depend on timing (fixed order of additions). */
 int lookm_chunk_attention(const void* q, const void* cache_k, const void* cache_v, const int* page_table,
                           const int* cu_seqlens_host, const int* cache_lens_host, int n_requests,

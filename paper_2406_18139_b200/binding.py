@@ -437,7 +437,7 @@ def _here(tensors) -> bool:
 
 def _table(t, paged: PagedLayout, n: int, lens, more=None) -> bool:
     """Whether `t` holds page numbers, as the layout has it, for n requests of these many rows (and `more` of them: cu_seqlens)."""
-    if t.dtype is not _I32:
+    if t is None or t.dtype is not _I32:
         return False
     stride = paged.table_stride
     if t.stride() == (stride, 1) and t.nbytes >= 4 * n * stride and t.shape[1] == stride:

@@ -143,6 +143,7 @@ def test_tables_that_are_not_the_layouts(library, call):
         refused(library, call, **{name: wide[:, :4].contiguous()[:1]})
         refused(library, call, **{name: torch.zeros(4, 2, dtype=torch.int32).t()})
         refused(library, call, **{name: torch.zeros(8, dtype=torch.int32)})
+        refused(library, call, **{name: None})
         refused(library, call, **{name: table()[:, :2] if name == "page_table" else table()[:, :1]})
         taken(library, call, **{name: wide[:1]}, **one)      # one request: no other row is looked for
         taken(library, call, **{name: torch.zeros(1, 3, dtype=torch.int32)}, **one)          # fewer columns, and enough
