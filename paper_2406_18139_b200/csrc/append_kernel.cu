@@ -10,8 +10,9 @@
 // four and their partners in the rotation, so that no lane needs another's (eight consecutive ones of features that are not
 // rotated, or whose partner is the next one).  A CTA takes a few tokens; its threads first work out these tokens' cosines and
 // sines, which all heads share, then its warps take units of eight rows.
-//   21100 tokens x 40 heads (1.3 GB) 227 us = 5.7 TB/s, 0.87 of the copy rate; x 32 heads on 8 106 us.  Earlier: a row per half-warp at a time, in
-// order of heads, shuffles for the partners 370; four rows at a time, packed arithmetic 285.  Units of four rows 292, 3 CTAs per SM 245.
+//   21100 tokens x 40 heads (1.3 GB) 226 us = 5.7 TB/s, 0.88 of the copy rate, in a long row of calls 241 us; x 32 heads on 8 106 us.  700 tokens x 32
+// heads, inputs not in L2, 10.7 us; one token 3.3.  Earlier: a row per half-warp at a time, in order of heads, shuffles for the partners 370;
+// four rows at a time, packed arithmetic 285.  Units of four rows 292, 3 CTAs per SM 245.
 #include <algorithm>
 
 #include <cuda_bf16.h>

@@ -28,8 +28,8 @@
 // Slower: one issuing warp per stream (561: their products take turns and both streams wait longer), sixteen softmax warps with
 // half a row each (582: 104 registers do not do), exponentials partly on the FMA pipe (+3 to 7 %), the reference from the tiles
 // before so that exponentials need not wait for the maximum (500), polling instead of suspended waits (490).
-// Few query rows: memory.  Sixteen single tokens over 400 to 8192 rows, 32 heads on 8, 57 us = 4.9 TB/s; with weights, over 400 to
-// 16384, 109 us.
+// Few query rows: memory.  Sixteen single tokens over 400 to 8192 rows, 32 heads on 8, 57 us = 4.9 TB/s (58 in a long row of calls); with weights, over
+// 400 to 16384, 107 us (110).
 #include <algorithm>
 
 #include <cuda_bf16.h>

@@ -5,7 +5,7 @@
 // evict_select_kernel finds the rows (latency bound: four counting passes over keys that stay in registers), evict_copy_kernel and
 // evict_in_place_kernel move their keys, values and masses (HBM bound: every kept row read and written once).
 //   8192 rows x 8 heads down to 20 % 16 us (the launches' own cost is 6), 30000 x 8 29; sixteen caches of 1000 to 8192 rows x 32 heads down to
-// 80 % in place 349 us = 5.4 TB/s, 0.83 of the copy rate (rows, their pages and their numbers each waited for in turn: 752; two of the three asked
+// 80 % in place 349 us = 5.4 TB/s, 0.83 of the copy rate, in a long row of calls 352 (rows, their pages and their numbers each waited for in turn: 752; two of the three asked
 // for early 430; two or four rows a thread instead of three 350 and 429).
 #include <algorithm>
 
