@@ -318,7 +318,7 @@ int lookm_append_rows(const void* q, const void* k, const void* v, const int* po
  *   lse   [n_q_heads, tokens] fp32, natural-log row log-sum-exp; may be NULL
  *   cache_lens_host  rows of each cache with the new ones: at least as many as the new tokens
  * Logits, the softmax's maximum and sum, and the sums over the rows are fp32; probabilities are rounded to bf16 (2^-8 of each at most) for the
- * product with V, the result to bf16 once more.  Against 64 bits the two together are off by 2.2e-3 of the result's norm where values are
+ * product with V, the result to bf16 once more.  Against 64 bits the two together are off by up to 2.4e-3 of the result's norm where values are
  * independent, the last rounding alone by 1.7e-3.  lse and a step's weights have no part in either.
  * Results do not depend on timing (fixed order of additions). */
 int lookm_chunk_attention(const void* q, const void* cache_k, const void* cache_v, const int* page_table,
